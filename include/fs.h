@@ -149,8 +149,11 @@ typedef enum {
                                 elementwise ops and row reductions on the [B,M,D] result (operands: such
                                 values, per-row values, constants, inputs seen as [B,M,D]);
                                 what the hand-written FS_SCHED_BDOT_SOFTMAX kernel does not match */
-  FS_SCHED_TWO_STEP = 6      /* two generated kernels (fs_plan_create_two_step): reductions over whole tensors, then the
+  FS_SCHED_TWO_STEP = 6,     /* two generated kernels (fs_plan_create_two_step): reductions over whole tensors, then the
                                 ops that read their results */
+  FS_SCHED_BLOCK_TABLES = 7, /* the operators around a paged cache: fs_plan_create_block_tables, */
+  FS_SCHED_ROTARY = 8,       /* fs_plan_create_rotary, */
+  FS_SCHED_PAGED_ATTENTION = 9 /* fs_plan_create_paged_attention */
 } fs_schedule;
 
 /* Build a plan from a fusion group.
@@ -400,6 +403,107 @@ fs_status fs_fusion_pattern_group_size(const fs_fusion* fusion, int32_t k, int32
                                        int32_t* n_outputs, int32_t* measured);
 fs_status fs_fusion_pattern_group(const fs_fusion* fusion, int32_t k, fs_op_desc* ops, int32_t* input_of,
                                   int32_t* output_of);
+
+/* ---- Operators around a paged cache of keys and values ----------------------------------
+ * The cache holds the keys (and, in a buffer of the same layout, the values) of many requests in blocks of
+ * `block_size` tokens, a power of two up to 1024.  A token's slot is block * block_size + its place in the block; a
+ * request's row of the block table names the blocks that hold its tokens, in order.  Element (block, head, place, d) lies
+ * at block * block_stride + head * head_stride + place * slot_stride + d; all three strides 0: dense
+ * [blocks, kv heads, block_size, head_dim].  They are counted in elements, as all strides here, and rows must not overlap.
+ *
+ * Lengths, tables and slots are device data, 32-bit integers, so a step needs no host round trip and can be captured into
+ * a graph; a plan holds what is the same for every step.  Plans are launched, described and destroyed like all others.
+ * What the data says is checked where it is used: a block number outside [0, blocks), a slot outside the cache or a length
+ * beyond a table's row never leads to an access outside the buffers (what it leads to is said below).
+ * fs_plan_info counts as algorithmic_bytes what a step moves whose requests fill their tables. */
+
+/* Block tables and slot maps from request lengths: the step that precedes the two operators below.
+ *   inputs    cached i32 [requests]   tokens each request has in the cache (below 0: 0; at most its row of the table)
+ *             fresh  i32 [requests]   tokens it is to get (below 0: 0), cut to what its row has room for; requests are
+ *                                     served in order until `tokens` is reached, the request there is cut, the others get none
+ *             free   i32 [free_blocks] blocks not in use, taken from the front
+ *   outputs   tables i32 [requests, table_blocks]  read and written: the entries behind the blocks that the cached tokens
+ *                                     take are appended as the new tokens need them, -1 where the free list is used up;
+ *                                     no other entry is touched
+ *             lengths i32 [requests]  cached + new tokens
+ *             starts i32 [requests+1] first row of each request's new tokens; the last entry is their number
+ *             positions, slots i32 [tokens]  of each row's token: its position in its request and its slot (-1 where its
+ *                                     block is outside [0, blocks)); rows behind the last token get 0 and -1
+ *             taken  i32 [2]          blocks taken from the free list, and blocks that were needed
+ * requests up to 4096, tokens up to 2^30, blocks * block_size and table_blocks * block_size below 2^31.
+ * Errors: FS_ERR_INVALID, FS_ERR_NOMEM. */
+typedef struct {
+  int32_t requests, tokens;
+  int32_t blocks, block_size;
+  int32_t table_blocks, free_blocks;
+} fs_block_tables_desc;
+fs_status fs_plan_create_block_tables(const fs_block_tables_desc* desc, fs_plan** out);
+
+/* Rotary positions.  Of every head of q [tokens, q_heads, head_dim] and k [tokens, k_heads, head_dim] the first
+ * rotary_dim elements are turned in pairs, (i, i + rotary_dim / 2) or, interleaved, (2i, 2i + 1), by the angle
+ * position * frequencies[i]; the others are copied:
+ *     y0 = magnitude * (x0 cos - x1 sin)     y1 = magnitude * (x1 cos + x0 sin)
+ * inverse: turned back (sin negated), which is the gradient of the same call with respect to q and k.
+ * The angle is formed in 64 bits, everything else in fp32, rounded once at the store.
+ *   inputs    q, k, positions i32 [tokens], frequencies f64 [rotary_dim / 2], radians (fs_rotary_frequencies)
+ *   outputs   q and k turned; either may take its own input's buffer where the two strides agree
+ * With blocks > 0 the keys go into the cache instead, and the values with them:
+ *   inputs    q, k, v [tokens, k_heads, head_dim], positions, frequencies, slots i32 [tokens]
+ *   outputs   q turned, k_cache, v_cache
+ *   A row whose slot is outside [0, blocks * block_size) is padding: nothing is written for it, not even q.  Two rows of
+ *   one call with the same slot leave the slot's contents undefined.
+ * Strides run from token to token, 0: dense; q, k and v may be parts of one packed projection (interleaved: even strides).
+ * FS_F32, FS_F16 or FS_BF16, head_dim and rotary_dim even, head_dim up to 512, k_heads 0 (without a cache): q alone, no k among inputs and outputs.
+ * Errors: FS_ERR_INVALID, FS_ERR_NOMEM. */
+typedef struct {
+  int32_t dtype;                   /* of q, k, v, their outputs and the cache */
+  int32_t tokens, q_heads, k_heads, head_dim, rotary_dim;
+  int32_t interleaved, inverse;    /* 0 or 1 */
+  int32_t blocks, block_size;      /* of the cache; blocks 0: none */
+  int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
+  int64_t block_stride, head_stride, slot_stride;
+  double magnitude;                /* finite; 1 where nothing scales */
+} fs_rotary_desc;
+fs_status fs_plan_create_rotary(const fs_rotary_desc* desc, fs_plan** out);
+
+/* The frequencies of a rotary embedding, rotary_dim / 2 doubles of host memory: base^(-2i / rotary_dim), stretched for
+ * contexts longer than `original` positions.  factor: what the positions are scaled down by; low and high 0: every
+ * frequency is divided by it; otherwise (0 < low < high) a wave that fits more than `high` times into `original` is kept, one
+ * that fits less than `low` times divided, those in between blended linearly in that number.
+ * Errors: FS_ERR_INVALID (base not above 0, factor below 1, original not above 0 where low and high are given). */
+fs_status fs_rotary_frequencies(int32_t rotary_dim, double base, double factor, double low, double high, double original, double* out);
+
+/* Attention of new tokens over the paged cache, which already holds their own keys and values.  Request b has
+ * lengths[b] keys, the last of them its new tokens, whose queries are rows starts[b] .. starts[b+1]-1 of q.  Query heads
+ * share key heads in runs of q_heads / kv_heads.  For the query at position p, over the keys j that it sees
+ *     s_j = scale * q . k_j      out = sum_j softmax(s)_j v_j      lse = log sum_j exp(s_j)
+ * causal: j <= p; with a window also j > p - window.  A row that sees no key gets zeros, and -inf as log-sum-exp.
+ *   inputs    q [tokens, q_heads, head_dim], k_cache, v_cache, tables i32 [requests, table_blocks], lengths i32 [requests],
+ *             starts i32 [requests+1]
+ *   outputs   out [tokens, q_heads, head_dim]; with log_sum_exp also lse f32 [tokens, q_heads]
+ *   partial_bytes  host, receives the size of the partial results of work that is split over the keys.  Where it is not
+ *             0 the caller gives fs_launch a device buffer of that size as ONE MORE OUTPUT, behind the others; nothing
+ *             in it has to start at zero, and launches with buffers of their own may overlap in time.
+ * Rows outside every request are left as they were.  A length beyond the table's row counts as that row's, one below 0 as 0;
+ * starts are cut to [0, tokens] and a run that ends before it begins is empty.  Keys in blocks outside [0, blocks) are not
+ * seen.  What lies in the cache behind a request's length is never used, whatever it is, and an infinity or NaN in a value
+ * reaches only the rows that see it.
+ * max_new: the most new tokens that a request has, for the choice of kernels (0: unknown); a request may have more.
+ * FS_F16 or FS_BF16 (the probabilities are rounded to it for the second product, all sums are fp32), head_dim 32, 64, 96 or
+ * 128, strides and head strides multiples of 8.  Results do not depend on timing: no atomics, a fixed order of sums.
+ * Errors: FS_ERR_INVALID, FS_ERR_UNSUPPORTED (a head_dim or stride that no kernel takes), FS_ERR_NOMEM. */
+typedef struct {
+  int32_t dtype;                   /* FS_F16 or FS_BF16: q, caches, out */
+  int32_t requests, tokens, q_heads, kv_heads, head_dim;
+  int32_t blocks, block_size, table_blocks;
+  int32_t causal, window;          /* window 0: none; it needs causal */
+  int32_t max_new, log_sum_exp;
+  int32_t reserved;                /* must be 0 */
+  int64_t q_stride, out_stride;    /* from token to token, 0: dense */
+  int64_t block_stride, head_stride, slot_stride;
+  double scale;                    /* finite */
+} fs_paged_attention_desc;
+fs_status fs_plan_create_paged_attention(const fs_paged_attention_desc* desc, int64_t* partial_bytes, fs_plan** out);
 
 /* Measurement aid: plain streaming copy of `bytes` (multiple of 16) from src to dst,
  * both DEVICE pointers, 16-byte aligned, on `hip_stream`.  Gives the achievable HBM

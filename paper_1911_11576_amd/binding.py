@@ -21,7 +21,8 @@ LIB_PATH = os.environ.get("FS_LIB_PATH") or os.path.join(os.path.dirname(os.path
 FS_OK, FS_ERR_INVALID, FS_ERR_UNSUPPORTED, FS_ERR_LDS, FS_ERR_HIP, FS_ERR_NOMEM = range(6)
 STATUS_NAMES = ["FS_OK", "FS_ERR_INVALID", "FS_ERR_UNSUPPORTED", "FS_ERR_LDS", "FS_ERR_HIP", "FS_ERR_NOMEM"]
 FS_MODE_STITCHED, FS_MODE_PER_OP, FS_MODE_STITCHED_PREBUILT, FS_MODE_STITCHED_GENERATED = 0, 1, 2, 3
-SCHEDULE_NAMES = ["per_op", "row", "row_col", "bdot_softmax", "elementwise", "block_dot", "two_step"]
+SCHEDULE_NAMES = ["per_op", "row", "row_col", "bdot_softmax", "elementwise", "block_dot", "two_step", "block_tables", "rotary",
+                  "paged_attention"]
 
 DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
 OPKINDS = {name: i for i, name in enumerate((
@@ -46,6 +47,23 @@ class fs_fusion_options(C.Structure):
                 ("seed_bytes", C.c_int64), ("bw_bytes", C.POINTER(C.c_int64)), ("bw_gbs", C.POINTER(C.c_double)),
                 ("n_bw", C.c_int32), ("n_extra", C.c_int32), ("extra_sizes", C.POINTER(C.c_int32)),
                 ("extra_ops", C.POINTER(C.c_int32)), ("extra_scores", C.POINTER(C.c_double))]
+
+
+class fs_block_tables_desc(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("requests", "tokens", "blocks", "block_size", "table_blocks", "free_blocks")]
+
+
+class fs_rotary_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "tokens", "q_heads", "k_heads", "head_dim", "rotary_dim", "interleaved", "inverse",
+                                          "blocks", "block_size")] +
+                [(n, C.c_int64) for n in ("q_stride", "k_stride", "v_stride", "q_out_stride", "k_out_stride",
+                                          "block_stride", "head_stride", "slot_stride")] + [("magnitude", C.c_double)])
+
+
+class fs_paged_attention_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "requests", "tokens", "q_heads", "kv_heads", "head_dim", "blocks", "block_size", "table_blocks",
+                                          "causal", "window", "max_new", "log_sum_exp", "reserved")] +
+                [(n, C.c_int64) for n in ("q_stride", "out_stride", "block_stride", "head_stride", "slot_stride")] + [("scale", C.c_double)])
 
 
 class FsError(RuntimeError):
@@ -132,6 +150,14 @@ def lib():
         L.fs_fusion_pattern_group_size.restype = i32
         L.fs_fusion_pattern_group.argtypes = [vp, i32, C.POINTER(fs_op_desc), C.POINTER(i32), C.POINTER(i32)]
         L.fs_fusion_pattern_group.restype = i32
+        L.fs_plan_create_block_tables.argtypes = [C.POINTER(fs_block_tables_desc), C.POINTER(vp)]
+        L.fs_plan_create_block_tables.restype = i32
+        L.fs_plan_create_rotary.argtypes = [C.POINTER(fs_rotary_desc), C.POINTER(vp)]
+        L.fs_plan_create_rotary.restype = i32
+        L.fs_rotary_frequencies.argtypes = [i32] + [C.c_double] * 5 + [C.POINTER(C.c_double)]
+        L.fs_rotary_frequencies.restype = i32
+        L.fs_plan_create_paged_attention.argtypes = [C.POINTER(fs_paged_attention_desc), C.POINTER(i64), C.POINTER(vp)]
+        L.fs_plan_create_paged_attention.restype = i32
         _native = _launch_calls(L)
         _lib = L
     return _lib
@@ -236,6 +262,48 @@ def fs_plan_create_two_step(ops):
     arr = ops if isinstance(ops, C.Array) else marshal_ops(ops)
     nbytes, out = C.c_int64(), C.c_void_p()
     _check(lib().fs_plan_create_two_step(arr, len(arr), C.byref(nbytes), C.byref(out)))
+    return out.value, nbytes.value
+
+
+# ---- the operators around a paged cache of keys and values: shapes, rules and orders of inputs and outputs are in include/fs.h
+
+def fs_plan_create_block_tables(requests, tokens, blocks, block_size, table_blocks, free_blocks):
+    """-> plan handle.  Inputs cached, fresh, free; outputs tables (updated in place), lengths, starts, positions, slots,
+    taken; all int32."""
+    out = C.c_void_p()
+    _check(lib().fs_plan_create_block_tables(C.byref(fs_block_tables_desc(requests, tokens, blocks, block_size, table_blocks, free_blocks)), C.byref(out)))
+    return out.value
+
+
+def fs_plan_create_rotary(dtype, tokens, q_heads, k_heads, head_dim, rotary_dim=None, interleaved=False, inverse=False, magnitude=1.0,
+                          q_stride=0, k_stride=0, v_stride=0, q_out_stride=0, k_out_stride=0, blocks=0, block_size=0, block_stride=0,
+                          head_stride=0, slot_stride=0):
+    """-> plan handle.  Inputs q, k, positions (int32), frequencies (float64, see fs_rotary_frequencies); outputs q and k
+    turned.  With blocks: inputs q, k, v, positions, frequencies, slots; outputs q, k_cache, v_cache.  Strides in elements
+    from token to token, 0: dense.  inverse: the gradient of the same call."""
+    d = fs_rotary_desc(DTYPES[dtype], tokens, q_heads, k_heads, head_dim, head_dim if rotary_dim is None else rotary_dim, int(interleaved), int(inverse),
+                       blocks, block_size, q_stride, k_stride, v_stride, q_out_stride, k_out_stride, block_stride, head_stride, slot_stride, magnitude)
+    out = C.c_void_p()
+    _check(lib().fs_plan_create_rotary(C.byref(d), C.byref(out)))
+    return out.value
+
+
+def fs_rotary_frequencies(rotary_dim, base=10000.0, factor=1.0, low=0.0, high=0.0, original=0.0):
+    """-> rotary_dim / 2 floats, radians a position, stretched by `factor` for long contexts: all of them, or with low, high and
+    original only the long waves (include/fs.h)."""
+    buf = (C.c_double * max(1, rotary_dim // 2))()
+    _check(lib().fs_rotary_frequencies(rotary_dim, base, factor, low, high, original, buf))
+    return list(buf[:rotary_dim // 2])
+
+
+def fs_plan_create_paged_attention(dtype, requests, tokens, q_heads, kv_heads, head_dim, blocks, block_size, table_blocks, scale, causal=True,
+                                   window=0, max_new=0, lse=False, q_stride=0, out_stride=0, block_stride=0, head_stride=0, slot_stride=0):
+    """-> (plan handle, bytes of the partial results, for which the plan takes a buffer as one more output; 0: none).  Inputs
+    q, k_cache, v_cache, tables, lengths, starts (int32); outputs out, with lse also the log-sum-exp (float32)."""
+    d = fs_paged_attention_desc(DTYPES[dtype], requests, tokens, q_heads, kv_heads, head_dim, blocks, block_size, table_blocks, int(causal), window, max_new,
+                                int(lse), 0, q_stride, out_stride, block_stride, head_stride, slot_stride, scale)
+    nbytes, out = C.c_int64(), C.c_void_p()
+    _check(lib().fs_plan_create_paged_attention(C.byref(d), C.byref(nbytes), C.byref(out)))
     return out.value, nbytes.value
 
 
@@ -410,6 +478,22 @@ class Plan:
     def two_step(cls, ops):
         """fs_plan_create_two_step -> (plan, bytes of the buffer it takes as its last output)."""
         h, nbytes = fs_plan_create_two_step(ops)
+        return cls(None, _handle=h), nbytes
+
+    @classmethod
+    def block_tables(cls, *args, **kwargs):
+        """fs_plan_create_block_tables -> plan."""
+        return cls(None, _handle=fs_plan_create_block_tables(*args, **kwargs))
+
+    @classmethod
+    def rotary(cls, *args, **kwargs):
+        """fs_plan_create_rotary -> plan."""
+        return cls(None, _handle=fs_plan_create_rotary(*args, **kwargs))
+
+    @classmethod
+    def paged_attention(cls, *args, **kwargs):
+        """fs_plan_create_paged_attention -> (plan, bytes of the buffer it takes as its last output, 0: none)."""
+        h, nbytes = fs_plan_create_paged_attention(*args, **kwargs)
         return cls(None, _handle=h), nbytes
 
     @classmethod

@@ -474,6 +474,13 @@ extern "C" {
 // Arguments of a launch checked against the plan (counts, NULL and alignment, identical pointers).
 fs_status fs::check_launch_args(fs_plan* p, const void* const* inputs, int32_t n_in, void* const* outputs, int32_t n_out) {
   if (!p) return set_error(FS_ERR_INVALID, "plan is NULL");
+  if (p->paged.kind) {
+    try {
+      return fs::paged_check_args(p->paged, inputs, n_in, outputs, n_out);
+    } catch (...) {
+      return FS_ERR_INVALID;
+    }
+  }
   const fs::Graph& g = p->graph;
   if (n_in != (int32_t)g.params.size()) return set_error(FS_ERR_INVALID, "n_in differs from the number of parameters");
   const bool two_step = p->schedule == FS_SCHED_TWO_STEP;
@@ -543,6 +550,9 @@ fs_status fs::enqueue_plan(fs_plan* p, const void* const* inputs, void* const* o
       case FS_SCHED_BDOT_SOFTMAX: rc = fs::attn_stitch_launch(p->match.attn, p->attn, inputs, outputs, hip_stream, &err); break;
       case FS_SCHED_ELEMENTWISE: rc = fs::ew_stitch_launch(p->ew, inputs, outputs, n_out, hip_stream, &err); break;
       case FS_SCHED_TWO_STEP: rc = fs::two_step_launch(p->two_step, inputs, outputs, n_out - 1, outputs[n_out - 1], hip_stream, &err); break;
+      case FS_SCHED_BLOCK_TABLES:
+      case FS_SCHED_ROTARY:
+      case FS_SCHED_PAGED_ATTENTION: rc = fs::paged_launch(p->paged, inputs, outputs, hip_stream, &err); break;
       default: rc = fs::per_op_launch(p->graph, p->per_op, inputs, outputs, workspace, hip_stream, &err); break;
     }
     if (rc != 0) return set_error(FS_ERR_HIP, err);
@@ -711,7 +721,7 @@ fs_status fs_plan_info(const fs_plan* p, int32_t* schedule, int32_t* n_kernels, 
   if (n_kernels) *n_kernels = p->n_kernels;
   if (lds_bytes) *lds_bytes = p->lds_bytes;
   if (workspace_bytes) *workspace_bytes = p->workspace_bytes;
-  if (algorithmic_bytes) *algorithmic_bytes = p->graph.algorithmic_bytes();
+  if (algorithmic_bytes) *algorithmic_bytes = p->paged.kind ? p->paged.bytes : p->graph.algorithmic_bytes();
   if (moved_bytes) *moved_bytes = p->moved_bytes;
   return FS_OK;
 }

@@ -7,6 +7,7 @@
 #include "grid_codegen.h"
 #include "launchers.h"
 #include "match.h"
+#include "paged.h"
 #include "per_op.h"
 #include "row_codegen.h"
 
@@ -25,6 +26,7 @@ struct fs_plan {
   fs::EwLaunch ew;
   fs::TwoStepLaunch two_step;   // schedule FS_SCHED_TWO_STEP: takes one more output, the doubles between its two kernels
   fs::PerOpPlan per_op;
+  fs::PagedPlan paged;          // schedules FS_SCHED_BLOCK_TABLES and on: `graph` is empty
   int n_kernels = 1;
   int64_t lds_bytes = 0, workspace_bytes = 0, moved_bytes = 0;
   void* workspace = nullptr;
