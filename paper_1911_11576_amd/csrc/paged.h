@@ -26,6 +26,8 @@ struct PagedAttnSpec {
   fs_paged_attention_desc d{};
   CacheLayout cache;
   int share = 1;                   // query heads to a key head
+  int row_tiles = 1;               // few rows: 16-row tiles
+  int unit_keys = 128, log_groups = 0;
   int64_t partial_bytes = 0;
 };
 

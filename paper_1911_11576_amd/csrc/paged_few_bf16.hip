@@ -1,0 +1,6 @@
+// Attention over a paged cache, few rows a request: bf16.
+#include "paged_few_impl.h"
+
+namespace fs {
+hipError_t paged_few_launch_bf16(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) { return paged_few_launch_type<bf16_t>(a, dim, row_tiles, s); }
+}  // namespace fs
