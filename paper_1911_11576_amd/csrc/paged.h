@@ -26,8 +26,11 @@ struct PagedAttnSpec {
   fs_paged_attention_desc d{};
   CacheLayout cache;
   int share = 1;                   // query heads to a key head
-  int row_tiles = 1;               // few rows: 16-row tiles
-  int unit_keys = 128, log_groups = 0;
+  // requests of up to few_rows rows: tiles of 16 * row_tiles, units of unit_keys keys, 1 << log_groups workgroups
+  int few_rows = 0, row_tiles = 1, unit_keys = 128, log_groups = 0;
+  // the others: places for tiles of 128 rows (0: there are none), parts of a tile's keys and their least length in steps of 64 keys
+  int64_t slots = 0, few_bytes = 0;
+  int most_parts = 1, least_steps = 1;
   int64_t partial_bytes = 0;
 };
 

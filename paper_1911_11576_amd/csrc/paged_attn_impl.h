@@ -22,6 +22,9 @@ struct PagedArgs {
   float scale2;                    // scale times log2 e: scores are kept in units of log 2
   int unit_keys;                   // few rows: keys of a unit of work, a multiple of 128
   int log_groups;                  // few rows: workgroups = 1 << log_groups
+  int few_rows;                    // requests of up to so many rows are the few-rows kernel's, the others the tile kernel's
+  float* tile_partial;             // tiles of 128 rows: [slots][kv_heads][most_parts][128 * (D + 2)]
+  int slots, most_parts, least_steps;      // places for tiles, parts that a tile's keys are split into at most, steps of 64 keys of a part at least
 };
 
 // A request as the kernels see it: its first row of q, its new tokens, its keys.
@@ -63,5 +66,8 @@ template <typename T> __device__ __forceinline__ u32x4 without_odd(u32x4 v) {
 // few rows a request: the work split evenly over a fixed grid, then the parts joined
 hipError_t paged_few_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 hipError_t paged_few_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+// many rows a request: tiles of 128
+hipError_t paged_tile_launch_f16(const PagedArgs&, int dim, hipStream_t);
+hipError_t paged_tile_launch_bf16(const PagedArgs&, int dim, hipStream_t);
 
 }  // namespace fs

@@ -36,7 +36,7 @@ template <int NT> struct FewLine {
     units = 0;
     if (b < a.requests) {
       mine = paged_request(a, b);
-      units = (uint32_t)((mine.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(mine) * (uint32_t)a.kv_heads;
+      if (mine.fresh * a.share <= a.few_rows) units = (uint32_t)((mine.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(mine) * (uint32_t)a.kv_heads;
     }
     upto = units;
 #pragma unroll
