@@ -39,7 +39,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     if (wgs * s->most_parts > 0x7fffffffll) { *err = "too many tiles for one grid"; return false; }
     if (s->most_parts > 1 && s->partial_bytes) s->partial_bytes += wgs * s->most_parts * 128 * (d.head_dim + 2) * 4;
     *n_kernels = s->most_parts > 1 ? 4 : 3;
-    *lds_bytes = std::max<int64_t>(*lds_bytes, 2ll * 64 * 2 * (2 * d.head_dim + 8 + 32) + 32);
+    *lds_bytes = std::max<int64_t>(*lds_bytes, 2ll * 64 * 2 * 2 * d.head_dim + 48);
   }
   return true;
 }
@@ -64,6 +64,7 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.requests = s.d.requests; a.tokens = s.d.tokens; a.q_heads = s.d.q_heads; a.kv_heads = s.d.kv_heads; a.share = s.share; a.causal = s.d.causal; a.window = s.d.window;
   a.width = s.d.blocks ? s.d.table_blocks : 0;      // (without a block there is no key to see, and no address to read)
   a.scale2 = (float)(s.d.scale * 1.4426950408889634);
+  if (a.scale2 == 0.f) a.scale2 = 1.17549435e-38f;      // (what is not seen is -inf times the scale)
   a.unit_keys = s.unit_keys; a.log_groups = s.log_groups;
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.few_rows = s.few_rows;

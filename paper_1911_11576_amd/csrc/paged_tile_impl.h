@@ -19,6 +19,16 @@ template <> __device__ __forceinline__ f32x16 mfma32<bf16_t>(u32x4 a, u32x4 b, f
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
+// 16 bytes a lane from memory straight into LDS: piece I of 64 bytes of a lane's row to the wavefront's 1024 bytes at `lds` + 1024 I.
+// (The instruction's offset counts on both sides.  As assembly, since the compiler makes every LDS read behind the builtin wait for
+// all loads in flight, the next step's among them; there is no register that it writes.)
+template <int I> __device__ __forceinline__ void load_lds16(const uint16_t* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory");
+}
+// ... all of them there, before a barrier that hands them on
+__device__ __forceinline__ void wait_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
+
 template <class Op> __device__ __forceinline__ float halves_allreduce(float v) {
   const uint32_t u = as_u32(v);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
@@ -56,11 +66,18 @@ __device__ __forceinline__ bool tile_work(const PagedArgs& a, int slot, TileWork
   return true;
 }
 
+// 64 keys (or values) in LDS as the direct loads leave them: 16 keys to a wavefront's part, pieces of 64 bytes of them behind one
+// another, [key / 16][64-byte piece][key % 16][4 x 16 bytes].  The 16 bytes x of a piece of key r stand in place x ^ (r / 4 % 4): eight lanes that
+// read a 16-byte column, and the four rows of a transposing read, fall on different banks.
+template <int D> struct TileLds {
+  static constexpr int kPieces = D / 32, kKeys16 = 16 * D;      // halves of 16 keys
+  uint16_t v[64 * D];
+};
+
 template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_tile_kernel(const PagedArgs a) {
-  constexpr int KS = D / 16, DT = D / 32, CH = D / 32;      // CH: 16-byte pieces of a key's row that a thread stages
-  constexpr int KP = D + 8, VP = D == 96 ? D + 16 : D == 32 ? D + 16 : D + 32;      // rows in LDS (halves), padded against bank conflicts
-  __shared__ __align__(16) uint16_t ksh[2][64 * KP], vsh[2][64 * VP];
-  __shared__ uint32_t flags[2][4];                          // of 16 keys each: those that are there, and bit 16: odd values
+  constexpr int KS = D / 16, DT = D / 32, CH = D / 32, K16 = 16 * D;
+  __shared__ __align__(1024) TileLds<D> ksh[2], vsh[2];
+  __shared__ uint32_t flags[2][4], odds[4];                 // which of a wavefront's 16 keys are there; whether a value of them is infinite or NaN
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
   const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
@@ -108,70 +125,96 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
     for (int i = 0; i < 16; ++i) o[dt][i] = 0.f;
   float m = -INFINITY, l = 0.f;
 
-  // ---- staging: thread (key tid / 4, pieces tid % 4 + 4 i)
-  const int skey = tid >> 2, piece = (tid & 3) * 8;
-  const int64_t head_at = (int64_t)head * a.cache.head + piece;
+  // ---- staging: wavefront w brings keys 16w .. 16w + 15, four lanes to a key
+  const int srow = lane >> 2, skey = 16 * w + srow;
+  const int64_t head_at = (int64_t)head * a.cache.head + 8 * ((lane & 3) ^ (srow >> 2 & 3));
   const uint16_t *kbase = static_cast<const uint16_t*>(a.k) + head_at, *vbase = static_cast<const uint16_t*>(a.v) + head_at;
-  u32x4 kr[CH], vr[CH];
-  bool ok;
+  const int key_last = min(r.keys, key_first + 64 * steps);
   int block;
-  const int key_last = key_first + 64 * steps;
   auto request_block = [&](int key0) __attribute__((always_inline)) { block = table[max(0, min(key0 + skey, r.keys - 1)) >> a.cache.shift]; };
-  auto request_rows = [&](int key0) __attribute__((always_inline)) {
+  auto request_rows = [&](int key0, int buf) __attribute__((always_inline)) {
     const int key = key0 + skey;
-    ok = key < min(r.keys, key_last) && (unsigned)block < (unsigned)a.cache.blocks;
+    const bool ok = key < key_last && (unsigned)block < (unsigned)a.cache.blocks;
     const int64_t at = (int64_t)(ok ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) kr[i] = *reinterpret_cast<const u32x4*>(kbase + at + 32 * i);
-#pragma unroll
-    for (int i = 0; i < CH; ++i) vr[i] = *reinterpret_cast<const u32x4*>(vbase + at + 32 * i);
-  };
-  auto stage = [&](int key0, int buf) __attribute__((always_inline)) {
+    const uint32_t kl = lds_address(&ksh[buf].v[w * K16]), vl = lds_address(&vsh[buf].v[w * K16]);
+    load_lds16<0>(kbase + at, kl);
+    load_lds16<0>(vbase + at, vl);
+    if constexpr (CH > 1) { load_lds16<1>(kbase + at, kl); load_lds16<1>(vbase + at, vl); }
+    if constexpr (CH > 2) { load_lds16<2>(kbase + at, kl); load_lds16<2>(vbase + at, vl); }
+    if constexpr (CH > 3) { load_lds16<3>(kbase + at, kl); load_lds16<3>(vbase + at, vl); }
     const uint64_t good = __ballot(ok);
-    uint32_t flag = 0;
-    if (good != ~0ull || key0 + 64 > edge || key0 < edge2) {
-      uint32_t any = 0;
-#pragma unroll
-      for (int i = 0; i < CH; ++i) {
-        if (!ok) vr[i] = u32x4{0u, 0u, 0u, 0u};
-        any |= odd_values<T>(vr[i]);
-      }
-      if (__ballot(any != 0)) flag = 0x10000u;
+    uint32_t flag = 0xffffu;
+    if (good != ~0ull) {
+      flag = 0;
+      for (int k = 0; k < 16; ++k) flag |= (uint32_t)(good >> (4 * k) & 1) << k;
     }
-    // (four lanes to a key: every fourth bit)
-#pragma unroll
-    for (int k = 0; k < 16; ++k) flag |= (uint32_t)(good >> (4 * k) & 1) << k;
     if (lane == 0) flags[buf][w] = flag;
-#pragma unroll
-    for (int i = 0; i < CH; ++i) *reinterpret_cast<u32x4*>(&ksh[buf][skey * KP + piece + 32 * i]) = kr[i];
-#pragma unroll
-    for (int i = 0; i < CH; ++i) *reinterpret_cast<u32x4*>(&vsh[buf][skey * VP + piece + 32 * i]) = vr[i];
   };
 
   auto compute = [&](int key0, int buf) __attribute__((always_inline)) {
-    const uint32_t f0 = flags[buf][0], f1 = flags[buf][1], f2 = flags[buf][2], f3 = flags[buf][3];
-    const uint32_t valid0 = __builtin_amdgcn_readfirstlane((f0 & 0xffffu) | f1 << 16), valid1 = __builtin_amdgcn_readfirstlane((f2 & 0xffffu) | f3 << 16);
-    const bool odd = __builtin_amdgcn_readfirstlane((f0 | f1 | f2 | f3) >> 16) & 1;
-    const bool plain = (valid0 & valid1) == 0xffffffffu && key0 + 64 <= least && key0 >= latest;
+    const uint32_t valid0 = __builtin_amdgcn_readfirstlane(flags[buf][0] | flags[buf][1] << 16), valid1 = __builtin_amdgcn_readfirstlane(flags[buf][2] | flags[buf][3] << 16);
+    const bool there = (valid0 & valid1) == 0xffffffffu;
+    const bool idle = key0 >= most || key0 + 64 <= first;      // none of the wavefront's rows sees any
+    if (!there || key0 + 64 > edge || key0 < edge2) {
+      // not every row sees every key: values of keys that are none do not count, whatever lies there; an infinity or NaN of another
+      // is added as it is in the rows that see it, and the dot runs without it
+      const bool ok = (flags[buf][w] >> srow & 1) != 0;
+      uint32_t any = 0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) {
+        u32x4* v = reinterpret_cast<u32x4*>(&vsh[buf].v[w * K16 + 512 * i + 8 * lane]);
+        if (!ok) *v = u32x4{0u, 0u, 0u, 0u};
+        else any |= odd_values<T>(*v);
+      }
+      const bool mine = __ballot(any != 0) != 0;
+      if (lane == 0) odds[w] = mine;
+      __syncthreads();
+      if (__builtin_amdgcn_readfirstlane(odds[0] | odds[1] | odds[2] | odds[3])) {
+        for (int k = 0; k < 64; ++k) {
+          const bool seen = ((k < 32 ? valid0 >> k : valid1 >> (k - 32)) & 1) && key0 + k < until && key0 + k >= from;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const u32x2 v = *reinterpret_cast<const u32x2*>(&vsh[buf].v[(k >> 4) * K16 + 512 * dt + (k & 15) * 32 + 8 * (j ^ (k >> 2 & 3)) + 4 * h]);
+              const float x[4] = {Mfma<T>::lo(v[0]), Mfma<T>::hi(v[0]), Mfma<T>::lo(v[1]), Mfma<T>::hi(v[1])};
+#pragma unroll
+              for (int i = 0; i < 4; ++i) o[dt][4 * j + i] += seen && !(fabsf(x[i]) < INFINITY) ? x[i] : 0.f;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < CH; ++i) {
+          u32x4* v = reinterpret_cast<u32x4*>(&vsh[buf].v[w * K16 + 512 * i + 8 * lane]);
+          *v = without_odd<T>(*v);
+        }
+        __syncthreads();
+      }
+    }
+    if (idle) return;
+    const bool plain = there && key0 + 64 <= least && key0 >= latest;
     // ---- S^T: 64 keys x 32 rows
     f32x16 s[2];
-    const uint16_t* klane = &ksh[buf][c * KP + 8 * h];
+    const uint16_t* klane = &ksh[buf].v[(c >> 4) * K16 + (c & 15) * 32];
+    const int kx = c >> 2 & 3;
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) s[t][i] = 0.f;
-#pragma unroll
-      for (int ks = 0; ks < KS; ++ks) s[t] = mfma32<T>(*reinterpret_cast<const u32x4*>(klane + 32 * t * KP + 16 * ks), qf[ks], s[t]);
-    }
+      for (int t = 0; t < 2; ++t) {
+        const u32x4 kf = *reinterpret_cast<const u32x4*>(klane + 2 * t * K16 + 512 * (ks / 2) + 8 * ((2 * (ks & 1) + h) ^ kx));
+        s[t] = ks == 0 ? mfma32<T>(kf, qf[0], f32x16{}) : mfma32<T>(kf, qf[ks], s[t]);
+      }
     // ---- softmax: the lane holds keys 32t + 8(i/4) + 4h + i%4 of its row
     if (!plain) {
+      // a bit for every key that the row sees, from the lane's first on
+      auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
+      for (int t = 0; t < 2; ++t) {
+        const int key = key0 + 32 * t;
+        const uint32_t see = ((t ? valid1 : valid0) & below(until - key) & ~below(from - key)) >> (4 * h);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int k = 8 * (i / 4) + 4 * h + i % 4, key = key0 + 32 * t + k;
-          if (!((t ? valid1 : valid0) >> k & 1) || key >= until || key < from) s[t][i] = -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i) s[t][i] = see & 1u << (8 * (i / 4) + i % 4) ? s[t][i] : -INFINITY;
+      }
     }
     float top = -INFINITY;
 #pragma unroll
@@ -196,8 +239,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
     for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float e = __builtin_amdgcn_exp2f(fmaf(s[t][i], scale2, -low));
-        if (!plain && s[t][i] == -INFINITY) e = 0.f;
+        const float e = __builtin_amdgcn_exp2f(fmaf(s[t][i], scale2, -low));
         s[t][i] = e;
         sum += e;
       }
@@ -208,58 +250,38 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
 #pragma unroll
       for (int i = 0; i < 4; ++i) pb[k][i] = Mfma<T>::pack(s[k / 2][8 * (k & 1) + 2 * i], s[k / 2][8 * (k & 1) + 2 * i + 1]);
     // ---- O^T += V^T . P^T
-    const int group = lane >> 4, cc = lane & 15;
-    const uint16_t* vlane = &vsh[buf][(4 * (group >> 1) + (cc >> 2)) * VP + 16 * (group & 1) + 4 * (cc & 3)];
+    // (keys 16k + 4h + 0 .. 3, and 8 behind them: places x ^ h and x ^ (h + 2))
+    const int cc = lane & 15;
+    const uint16_t* vlane = &vsh[buf].v[(4 * h + (cc >> 2)) * 32 + 4 * (cc & 1)];
+    const int vx = 2 * (lane >> 4 & 1) + (cc >> 1 & 1);
     auto vfrag = [&](int k, int dt) __attribute__((always_inline)) {
       typedef short s16x4 __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-      const uint16_t* p = vlane + 16 * k * VP + 32 * dt;
-      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p)));
-      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * VP)));
+      const uint16_t* p = vlane + k * K16 + 512 * dt;
+      const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 8 * (vx ^ h))));
+      const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(p + 256 + 8 * (vx ^ (h + 2)))));
       return u32x4{lo[0], lo[1], hi[0], hi[1]};
     };
-    if (!odd) {
-#pragma unroll
-      for (int k = 0; k < 4; ++k)
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32<T>(vfrag(k, dt), pb[k], o[dt]);
-      return;
-    }
-    // rows that see an infinite or NaN value get it as it is; the second dot runs without them
-    for (int k = 0; k < 64; ++k) {
-      if (!((k < 32 ? valid0 >> k : valid1 >> (k - 32)) & 1)) continue;
-      const bool seen = key0 + k < until && key0 + k >= from;
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const u32x2 v = *reinterpret_cast<const u32x2*>(&vsh[buf][k * VP + 32 * dt + 8 * j + 4 * h]);
-          const float x[4] = {Mfma<T>::lo(v[0]), Mfma<T>::hi(v[0]), Mfma<T>::lo(v[1]), Mfma<T>::hi(v[1])};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (seen && !(fabsf(x[i]) < INFINITY)) o[dt][4 * j + i] += x[i];
-        }
-    }
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
-      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32<T>(without_odd<T>(vfrag(k, dt)), pb[k], o[dt]);
+      for (int dt = 0; dt < DT; ++dt) o[dt] = mfma32<T>(vfrag(k, dt), pb[k], o[dt]);
   };
 
   if (steps > 0) {
     request_block(key_first);
-    request_rows(key_first);
+    request_rows(key_first, 0);
     request_block(key_first + 64);
-    stage(key_first, 0);
+    wait_lds_loads();
     __syncthreads();
     for (int i = 0; i < steps; ++i) {
       const int key0 = key_first + 64 * i;
       if (i + 1 < steps) {
-        request_rows(key0 + 64);
+        request_rows(key0 + 64, (i + 1) & 1);
         request_block(key0 + 128);
       }
-      if (key0 < most && key0 + 64 > first) compute(key0, i & 1);
-      if (i + 1 < steps) stage(key0 + 64, (i + 1) & 1);
+      compute(key0, i & 1);
+      wait_lds_loads();
       __syncthreads();
     }
   }
