@@ -14,31 +14,36 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   // rows to a tile of the few-rows kernel: 16 where that is what a request has, else 32
   s->row_tiles = (many ? s->share : rows) <= 16 ? 1 : 2;
   s->few_rows = many ? 16 * s->row_tiles : 1 << 30;
-  s->log_groups = 9;
-  s->unit_keys = 128;
-  // units are numbered in 31 bits
-  const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;
-  while (tiles * (keys / s->unit_keys + 1) > 0x7fffffffll) {
-    if (s->unit_keys >= (1 << 29)) { *err = "too many rows"; return false; }
-    s->unit_keys *= 2;
-  }
+  const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;      // at most
   const int64_t m = 16 * s->row_tiles;
-  s->few_bytes = d.tokens && d.requests ? (2ll << s->log_groups) * m * (d.head_dim + 2) * 4 : 0;
+  s->few_bytes = 0;
+  if (keys <= 1024 && tiles <= 65536) {
+    // no request is longer than four steps: a workgroup each tile, nothing to join
+    s->log_groups = -1;
+    s->unit_keys = 1024;
+    s->few_grid = (int)tiles;
+  } else {
+    s->log_groups = 8;
+    s->few_grid = 1 << s->log_groups;
+    s->unit_keys = 256;
+    // units are numbered in 31 bits
+    while (tiles * (keys / s->unit_keys + 1) > 0x7fffffffll) {
+      if (s->unit_keys >= (1 << 29)) { *err = "too many rows"; return false; }
+      s->unit_keys *= 2;
+    }
+    if (d.tokens && d.requests) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
+  }
   s->partial_bytes = s->few_bytes;
-  *n_kernels = 2;
+  *n_kernels = s->log_groups < 0 ? 1 : 2;
   const int64_t pad = d.head_dim == 64 ? 8 : 16;
-  *lds_bytes = std::max<int64_t>(4 * 32 * (d.head_dim + pad) * 2, 4 * m * (d.head_dim + 4) * 4) + 32 * m;
+  *lds_bytes = std::max<int64_t>(8 * 32 * (d.head_dim + pad) * 2, 8 * m * (d.head_dim + 4) * 4) + 64 * m;
   s->slots = 0;
-  s->most_parts = 1;
-  s->least_steps = 8;
   if (many) {
     s->slots = ((int64_t)d.tokens * s->share >> 7) + d.requests;
-    const int64_t wgs = s->slots * d.kv_heads;
-    // few tiles: their keys are split too, to about two workgroups a CU
-    s->most_parts = (int)std::max<int64_t>(1, std::min<int64_t>(512 / std::max<int64_t>(wgs, 1), (keys >> 6) / s->least_steps));
-    if (wgs * s->most_parts > 0x7fffffffll) { *err = "too many tiles for one grid"; return false; }
-    if (s->most_parts > 1 && s->partial_bytes) s->partial_bytes += wgs * s->most_parts * 128 * (d.head_dim + 2) * 4;
-    *n_kernels = s->most_parts > 1 ? 4 : 3;
+    if (s->slots * d.kv_heads > 0x7ffffbffll) { *err = "too many tiles for one grid"; return false; }
+    const bool ordered = d.requests <= 64;
+    if (ordered && d.tokens && d.requests) s->partial_bytes += 2ll * kTileShares * 128 * (d.head_dim + 2) * 4;
+    *n_kernels += ordered ? 2 : 1;
     *lds_bytes = std::max<int64_t>(*lds_bytes, 2ll * 64 * 2 * 2 * d.head_dim + 48);
   }
   return true;
@@ -46,8 +51,8 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
 
 std::string paged_attn_describe(const PagedAttnSpec& s) {
   char buf[320];
-  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=256; join[GRID,CTA]", 16 * s.row_tiles, s.unit_keys, 1 << s.log_groups);
-  if (s.slots) snprintf(buf + n, sizeof buf - n, "; requests of more than %d rows: rows to a tile=128, cta_num=%lld, parts=%d", s.few_rows, (long long)(s.slots * s.d.kv_heads * s.most_parts), s.most_parts);
+  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=512%s", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.log_groups < 0 ? "" : "; join[GRID,CTA]");
+  if (s.slots) snprintf(buf + n, sizeof buf - n, "; requests of more than %d rows: rows to a tile=128, cta_num=%lld", s.few_rows, (long long)(s.slots * s.d.kv_heads));
   return buf;
 }
 
@@ -60,16 +65,16 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   if (s.d.log_sum_exp) a.lse = static_cast<float*>(out[1]);
   a.q_stride = s.d.q_stride; a.out_stride = s.d.out_stride;
   a.cache = s.cache;
-  a.partial = static_cast<float*>(out[s.d.log_sum_exp ? 2 : 1]);
+  if (s.partial_bytes) a.partial = static_cast<float*>(out[s.d.log_sum_exp ? 2 : 1]);
   a.requests = s.d.requests; a.tokens = s.d.tokens; a.q_heads = s.d.q_heads; a.kv_heads = s.d.kv_heads; a.share = s.share; a.causal = s.d.causal; a.window = s.d.window;
   a.width = s.d.blocks ? s.d.table_blocks : 0;      // (without a block there is no key to see, and no address to read)
   a.scale2 = (float)(s.d.scale * 1.4426950408889634);
   if (a.scale2 == 0.f) a.scale2 = 1.17549435e-38f;      // (what is not seen is -inf times the scale)
-  a.unit_keys = s.unit_keys; a.log_groups = s.log_groups;
+  a.unit_keys = s.unit_keys; a.log_groups = s.log_groups; a.few_grid = s.few_grid;
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.few_rows = s.few_rows;
-  a.tile_partial = a.partial + s.few_bytes / 4;
-  a.slots = (int)s.slots; a.most_parts = s.most_parts; a.least_steps = s.least_steps;
+  if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;
+  a.slots = (int)s.slots; a.least_steps = s.least_steps;
   const bool f16 = s.d.dtype == FS_F16;
   hipError_t e = hipSuccess;
   if (s.slots) e = (f16 ? paged_tile_launch_f16 : paged_tile_launch_bf16)(a, s.d.head_dim, st);

@@ -20,12 +20,15 @@ struct PagedArgs {
   CacheLayout cache;
   int requests, tokens, q_heads, kv_heads, share, width, causal, window;
   float scale2;                    // scale times log2 e: scores are kept in units of log 2
-  int unit_keys;                   // few rows: keys of a unit of work, a multiple of 128
-  int log_groups;                  // few rows: workgroups = 1 << log_groups
+  int unit_keys;                   // few rows: keys of a unit of work, a multiple of 256
+  int log_groups, few_grid;        // few rows: workgroups, 1 << log_groups of them; log_groups -1: a unit each, which is a whole tile
   int few_rows;                    // requests of up to so many rows are the few-rows kernel's, the others the tile kernel's
-  float* tile_partial;             // tiles of 128 rows: [slots][kv_heads][most_parts][128 * (D + 2)]
-  int slots, most_parts, least_steps;      // places for tiles, parts that a tile's keys are split into at most, steps of 64 keys of a part at least
+  float* tile_partial;             // tiles of 128 rows: up to 2 * kTileShares of [128 * (D + 2)]
+  int slots, least_steps;          // places for tiles; steps of 64 keys that a tile may have in any case before it is split
 };
+
+// Workgroups of the tile kernel that the chip holds, two to a CU: what is shared out evenly.
+constexpr int kTileShares = 512;
 
 // A request as the kernels see it: its first row of q, its new tokens, its keys.
 struct PagedRequest { int first, fresh, keys; };
@@ -62,6 +65,24 @@ template <typename T> __device__ __forceinline__ u32x4 without_odd(u32x4 v) {
   }
   return v;
 }
+
+// 16 bytes a lane from memory straight into LDS: piece I of 64 bytes of a lane's row to the wavefront's 1024 bytes at `lds` + 1024 I.
+// (The instruction's offset counts on both sides.  As assembly, since the compiler makes every LDS read behind the builtin wait for
+// all loads in flight, the next step's among them; there is no register that it writes.  The code waits by itself, below.)
+// ONCE: read by nobody else, past the caches.
+template <int I, bool ONCE> __device__ __forceinline__ void load_lds16(const uint16_t* from, uint32_t lds) {
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2 nt" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory");
+}
+// 4 bytes a lane
+__device__ __forceinline__ void load_lds4(const int* from, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
+}
+// until all but the last N loads are there (they come in order)
+template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+// until LDS has been read: before a load writes there again
+__device__ __forceinline__ void wait_lds_reads() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
 
 // few rows a request: the work split evenly over a fixed grid, then the parts joined
 hipError_t paged_few_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);

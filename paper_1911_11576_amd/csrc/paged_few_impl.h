@@ -1,17 +1,19 @@
 // Attention over a paged cache, few rows a request (single tokens, a few guessed ones): bound by the reading of keys and values.
 //
 // The work of all requests is one line of units, (request, key head, tile of 16 * NT rows, run of keys), cut into as many equal
-// runs as there are workgroups: each finds its own from the lengths on the device, whatever their spread.  A workgroup's four
-// wavefronts take 32 keys each of every 128; a wavefront loads its keys straight into MFMA operands and its values through
-// registers into LDS of its own (no barrier in the loop), the next 32 keys' in flight meanwhile.  At the end of a tile's run the
+// runs as there are workgroups: each finds its own from the lengths on the device, whatever their spread.  A workgroup's
+// wavefronts take 32 keys each of a step; a wavefront brings keys and values into LDS of its own by direct loads of whole rows (no
+// barrier in the loop), the next 32 keys as soon as the first dot is through with these, their values behind the second.  At the end of a tile's run the
 // wavefronts' maxima, sums and results meet in LDS; a tile that one workgroup does from end to end is stored, parts of others go to
-// the partial results, which paged_few_join_kernel adds in the order of the keys.
+// the partial results, which paged_few_join_kernel adds in the order of the keys.  Where no request can be long a workgroup has
+// one tile and all of its keys, and nothing is left to join.
 #pragma once
 #include "paged_attn_impl.h"
 
 namespace fs {
 
-constexpr int kFewGroups = 9;      // log2 of the workgroups: two to a CU
+
+constexpr int kFewWaves = 8;      // of a workgroup, which is a CU's
 
 // Partial results of a workgroup: its first run of a tile and its last, each M rows of D sums, M maxima, M sums of exponentials.
 template <int D, int NT> struct FewPart { static constexpr int kRows = 16 * NT, kFloats = kRows * (D + 2); };
@@ -57,7 +59,9 @@ template <int NT> struct FewLine {
   // where workgroup p's run begins
   __device__ __forceinline__ uint32_t cut(int p, int log_groups) const { return (uint32_t)((uint64_t)p * total >> log_groups); }
   // log2 of the workgroups that have work: at least a unit each
-  __device__ __forceinline__ int groups() const { return min(a.log_groups, 31 - __clz((int)max(total, 1u))); }
+  __device__ __forceinline__ int groups() const {
+    return min(a.log_groups, 31 - __clz((int)max(total, 1u)));
+  }
   struct Tile { int b, head, row0, unit, n_units; uint32_t first; PagedRequest r; };      // first: the tile's first unit in the line
   __device__ __forceinline__ Tile find(uint32_t unit) {
     while (unit >= before + all && base + 64 < a.requests) {
@@ -80,23 +84,35 @@ template <int NT> struct FewLine {
   }
 };
 
-template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void paged_few_kernel(const PagedArgs a) {
-  constexpr int KS = D / 32, DT = D / 16, M = 16 * NT;
-  constexpr int VP = D + (D == 64 ? 8 : 16);       // row of V in LDS (halves), padded against bank conflicts
+// 32 rows of D halves in LDS as direct loads of whole rows leave them, 16 bytes x of row r in place x ^ f(r): eight lanes that read the
+// same 16 bytes of eight rows, and the four rows of a transposing read, fall on different banks.
+template <int D> __device__ __forceinline__ int few_turn(int row) { return D == 128 ? 2 * (row & 7) : D == 64 ? row & 6 : row >> 1 & 2; }
+
+template <typename T, int D, int NT> __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(const PagedArgs a) {
+  constexpr int W = kFewWaves, KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 32 * W, C = D / 8, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 32 rows
   constexpr int OP = D + 4;                        // row of results in LDS (floats)
-  constexpr int kLds = 4 * 32 * VP * 2 > 4 * M * OP * 4 ? 4 * 32 * VP * 2 : 4 * M * OP * 4;
-  __shared__ __align__(16) unsigned char smem[kLds];
-  __shared__ float ms[4][M], ls[4][M];
+  constexpr int kLds = W * 64 * D * 2 > W * M * OP * 4 ? W * 64 * D * 2 : W * M * OP * 4;
+  __shared__ __align__(1024) unsigned char smem[kLds];
+  __shared__ int blocks[W][2][64];                 // block numbers of the keys to come
+  __shared__ float ms[W][M], ls[W][M];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int c = lane & 15, g = lane >> 4;
-  uint16_t* vsh = reinterpret_cast<uint16_t*>(smem) + w * 32 * VP;
+  uint16_t *ksh = reinterpret_cast<uint16_t*>(smem) + w * 64 * D, *vsh = ksh + 32 * D;
+  const uint32_t k_lds = lds_address(ksh), v_lds = lds_address(vsh), b_lds = lds_address(&blocks[w][0][0]);
   float* osh = reinterpret_cast<float*>(smem);
 
   FewLine<NT> line(a);
   line.count();
-  const int log_groups = line.groups(), p = blockIdx.x;
-  if (p >> log_groups) return;
-  const uint32_t u0 = line.cut(p, log_groups), u1 = line.cut(p + 1, log_groups);
+  const int p = blockIdx.x;
+  uint32_t u0, u1;
+  if (a.log_groups < 0) {      // a unit is a tile, a workgroup has one
+    u0 = p; u1 = p + 1;
+    if (u0 >= line.total) return;
+  } else {
+    const int log_groups = line.groups();
+    if (p >> log_groups) return;
+    u0 = line.cut(p, log_groups); u1 = line.cut(p + 1, log_groups);
+  }
   const uint16_t *kbase = static_cast<const uint16_t*>(a.k), *vbase = static_cast<const uint16_t*>(a.v);
   const int in_block = (1 << a.cache.shift) - 1;
 
@@ -106,7 +122,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void p
     const PagedRequest r = tile.r;
     const int rows = r.fresh * a.share;
     const int* table = a.tables + (int64_t)tile.b * a.width;
-    const int64_t head_at = (int64_t)tile.head * a.cache.head + 8 * g;
+    const int64_t head_at = (int64_t)tile.head * a.cache.head;
     // ---- the rows: their queries as B operands, and the keys they see
     u32x4 qf[NT][KS];
     int until[NT], from[NT];
@@ -138,74 +154,59 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void p
     }
     const int key_first = paged_first_key(a, r) + tile.unit * a.unit_keys;
     const int key_end = min(most, key_first + n * a.unit_keys);
-    u32x4 vf[2][KS];      // values on their way to LDS
-    bool ok[2];           // the lane's two keys are there
-    uint32_t valid = 0;   // of 32 keys those that are there
-    bool plain, odd;      // every row sees every key; not so, and some value is infinite or NaN
-    // ---- 32 keys: the block numbers of the lane's two keys, then their rows
-    auto request_blocks = [&](int key0, int (&block)[2]) __attribute__((always_inline)) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) block[t] = table[min(key0 + 16 * t + c, r.keys - 1) >> a.cache.shift];
+    // ---- 32 keys: lane k's key has its row at `at`; load i brings piece (64 i + lane) % C of key (64 i + lane) / C
+    int block;
+    bool ok;
+    int64_t at;
+    auto block_of = [&](int key0) __attribute__((always_inline)) { return table + (min(key0 + lane, r.keys - 1) >> a.cache.shift); };
+    auto locate = [&](int key0) __attribute__((always_inline)) {
+      const int key = key0 + lane;
+      ok = key < key_end && (unsigned)block < (unsigned)a.cache.blocks;
+      at = head_at + (int64_t)(ok ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot;
     };
-    auto request_rows = [&](int key0, const int (&block)[2], u32x4 (&kf)[2][KS]) __attribute__((always_inline)) {
+    auto row_of = [&](int i) { return (64 * i + lane) / C; };
+    auto bring = [&](const uint16_t* base, uint32_t lds) __attribute__((always_inline)) {
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int key = key0 + 16 * t + c;
-        ok[t] = key < key_end && (unsigned)block[t] < (unsigned)a.cache.blocks;
-        const int64_t at = (int64_t)(ok[t] ? block[t] : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot + head_at;
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) kf[t][ks] = *reinterpret_cast<const u32x4*>(kbase + at + 32 * ks);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) vf[t][ks] = *reinterpret_cast<const u32x4*>(vbase + at + 32 * ks);
+      for (int i = 0; i < N; ++i) {
+        const int row = row_of(i), piece = (64 * i + lane) % C ^ few_turn<D>(row);
+        load_lds16<0, true>(base + __shfl((long long)at, row) + 8 * piece, lds + 1024 * i);
       }
     };
-    const uint16_t* vlane = vsh + (4 * g + (c >> 2)) * VP + 4 * (c & 3);
-    auto stage = [&](int key0) __attribute__((always_inline)) {
-      valid = (uint32_t)(__ballot(ok[0]) & 0xffffu) | (uint32_t)(__ballot(ok[1]) & 0xffffu) << 16;
-      plain = valid == 0xffffffffu && key0 + 32 <= least && key0 >= latest;
-      odd = false;
-      if (!plain) {
-        // keys that are none: their values do not count, whatever lies there; infinities and NaN of the others are for the rows that see them
-        uint32_t any = 0;
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            if (!ok[t]) vf[t][ks] = u32x4{0u, 0u, 0u, 0u};
-            any |= odd_values<T>(vf[t][ks]);
-          }
-        odd = __ballot(any != 0) != 0;
-      }
+    const int kturn = few_turn<D>(c), vturn = few_turn<D>(4 * g + (c >> 2));
+    const uint16_t *klane = ksh + c * D, *vlane = vsh + (4 * g + (c >> 2)) * D + 4 * (c & 1);
+    auto work = [&](int key0, int turn) __attribute__((always_inline)) {
+      const uint32_t valid = (uint32_t)__ballot(ok);                                        // of 32 keys those that are there
+      const bool plain = valid == 0xffffffffu && key0 + 32 <= least && key0 >= latest;      // every row sees every one
+      const bool more = key0 + KEYS < key_end;
+      wait_loads<N>();      // the keys are there (the values may not be)
+      f32x4 s[NT][2];
 #pragma unroll
       for (int t = 0; t < 2; ++t)
 #pragma unroll
-        for (int ks = 0; ks < KS; ++ks) *reinterpret_cast<u32x4*>(vsh + (16 * t + c) * VP + 32 * ks + 8 * g) = vf[t][ks];
-    };
-    auto work = [&](int key0, const u32x4 (&kf)[2][KS]) __attribute__((always_inline)) {
-      f32x4 s[NT][2];
+        for (int ks = 0; ks < KS; ++ks) {
+          const u32x4 kf = *reinterpret_cast<const u32x4*>(klane + 16 * t * D + 8 * ((4 * ks + g) ^ kturn));
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          s[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-          for (int ks = 0; ks < KS; ++ks) s[nt][t] = Mfma<T>::run(kf[t][ks], qf[nt][ks], s[nt][t]);
+          for (int nt = 0; nt < NT; ++nt) s[nt][t] = Mfma<T>::run(kf, qf[nt][ks], ks == 0 ? f32x4{0.f, 0.f, 0.f, 0.f} : s[nt][t]);
         }
+      if (more) {
+        block = blocks[w][turn][lane];
+        locate(key0 + KEYS);
+        wait_lds_reads();
+        load_lds4(block_of(key0 + 2 * KEYS), b_lds + 256 * (turn ^ 1));
+        bring(kbase, k_lds);
+      }
       u32x4 pb[NT];
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float top = m[nt];
-        bool seen[2][4];
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int k = 16 * t + 4 * g + i;
             float z = s[nt][t][i] * a.scale2;
-            seen[t][i] = true;
             if (!plain) {
-              seen[t][i] = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt];
-              z = seen[t][i] ? z : -INFINITY;
+              z = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt] ? z : -INFINITY;
             }
             s[nt][t][i] = z;
             top = fmaxf(top, z);
@@ -229,62 +230,65 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void p
           for (int i = 0; i < 4; ++i) o[nt][dt][i] *= keep;
         pb[nt] = u32x4{Mfma<T>::pack(s[nt][0][0], s[nt][0][1]), Mfma<T>::pack(s[nt][0][2], s[nt][0][3]), Mfma<T>::pack(s[nt][1][0], s[nt][1][1]), Mfma<T>::pack(s[nt][1][2], s[nt][1][3])};
       }
-      if (odd) {
-        // rows that see an infinite or NaN value get it as it is; the second dot then runs without them
-        for (int k = 0; k < 32; ++k) {
-          if (!(valid >> k & 1)) continue;
+      if (more) wait_loads<N + 1>();      // the values are there (the next keys may not be)
+      else wait_loads<0>();
+      if (!plain) {
+        // values of keys that are none do not count, whatever lies there; an infinity or NaN of another is added as it is in the
+        // rows that see it, and the second dot runs without it
+        uint32_t any = 0;
 #pragma unroll
-          for (int dt = 0; dt < DT; ++dt) {
-            const u32x2 v = *reinterpret_cast<const u32x2*>(vsh + k * VP + 16 * dt + 4 * g);
-            const float x[4] = {Mfma<T>::lo(v[0]), Mfma<T>::hi(v[0]), Mfma<T>::lo(v[1]), Mfma<T>::hi(v[1])};
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (key0 + k < until[nt] && key0 + k >= from[nt] && !(fabsf(x[i]) < INFINITY)) o[nt][dt][i] += x[i];
-          }
+        for (int i = 0; i < N; ++i) {
+          u32x4* v = reinterpret_cast<u32x4*>(vsh + 8 * (64 * i + lane));
+          if (!(valid >> row_of(i) & 1)) *v = u32x4{0u, 0u, 0u, 0u};
+          else any |= odd_values<T>(*v);
         }
+        if (__ballot(any != 0)) {
+          for (int k = 0; k < 32; ++k)
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+            for (int dt = 0; dt < DT; ++dt) {
+              const u32x2 v = *reinterpret_cast<const u32x2*>(vsh + k * D + 8 * ((2 * dt + (g >> 1)) ^ few_turn<D>(k)) + 4 * (g & 1));
+              const float x[4] = {Mfma<T>::lo(v[0]), Mfma<T>::hi(v[0]), Mfma<T>::lo(v[1]), Mfma<T>::hi(v[1])};
 #pragma unroll
-          for (int ks = 0; ks < KS; ++ks) {
-            u32x4* v = reinterpret_cast<u32x4*>(vsh + (16 * t + c) * VP + 32 * ks + 8 * g);
+              for (int nt = 0; nt < NT; ++nt) {
+                const bool seen = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[nt][dt][i] += seen && !(fabsf(x[i]) < INFINITY) ? x[i] : 0.f;
+              }
+            }
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            u32x4* v = reinterpret_cast<u32x4*>(vsh + 8 * (64 * i + lane));
             *v = without_odd<T>(*v);
           }
+        }
       }
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         typedef short s16x4 __attribute__((ext_vector_type(4)));
         typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
-        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vlane + 16 * dt)));
-        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(vlane + 16 * dt + 16 * VP)));
+        const uint16_t* v = vlane + 8 * ((2 * dt + (c >> 1 & 1)) ^ vturn);
+        const u32x2 lo = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)v));
+        const u32x2 hi = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)(v + 16 * D)));
         const u32x4 vt = {lo[0], lo[1], hi[0], hi[1]};
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) o[nt][dt] = Mfma<T>::run(vt, pb[nt], o[nt][dt]);
       }
+      if (more) {
+        wait_lds_reads();
+        bring(vbase, v_lds);
+      }
     };
-    // ---- the loop: this wavefront's 32 of every 128 keys, the next ones' loads in flight
+    // ---- the loop: this wavefront's 32 of every 256 keys, the next ones' loads in flight
     int key = key_first + 32 * w;
     if (key < key_end) {
-      u32x4 kf[2][2][KS];
-      int block[2];
-      request_blocks(key, block);
-      request_rows(key, block, kf[0]);
-      request_blocks(key + 128, block);
-      for (;;) {
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-          stage(key);
-          request_rows(key + 128, block, kf[half ^ 1]);
-          request_blocks(key + 256, block);
-          work(key, kf[half]);
-          key += 128;
-          if (key >= key_end) break;
-        }
-        if (key >= key_end) break;
-      }
+      block = *block_of(key);
+      locate(key);
+      load_lds4(block_of(key + KEYS), b_lds);
+      bring(kbase, k_lds);
+      bring(vbase, v_lds);
+      for (int turn = 0; key < key_end; key += KEYS, turn ^= 1) work(key, turn);
     }
-    // ---- the four wavefronts' results together
+    // ---- the wavefronts' results together
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       l[nt] = rows_allreduce<SumOp>(l[nt]);
@@ -294,7 +298,9 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void p
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       const int row = 16 * nt + c;
-      const float top = fmaxf(fmaxf(ms[0][row], ms[1][row]), fmaxf(ms[2][row], ms[3][row]));
+      float top = -INFINITY;
+#pragma unroll
+      for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
       const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - top);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
@@ -307,16 +313,17 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void p
     __syncthreads();
     const bool whole = n == tile.n_units;
     float* part = whole ? nullptr : a.partial + (int64_t)(2 * p + (cur == u0 ? 0 : 1)) * FewPart<D, NT>::kFloats;
-    for (int e = threadIdx.x; e < M * (D / 8); e += 256) {
+    for (int e = threadIdx.x; e < M * (D / 8); e += 64 * W) {
       const int row = e / (D / 8), d = e % (D / 8) * 8;
-      const float m0 = ms[0][row], m1 = ms[1][row], m2 = ms[2][row], m3 = ms[3][row], top = fmaxf(fmaxf(m0, m1), fmaxf(m2, m3)), low = top == -INFINITY ? 0.f : top;
-      const float sum = ls[0][row] * __builtin_amdgcn_exp2f(m0 - low) + ls[1][row] * __builtin_amdgcn_exp2f(m1 - low) + ls[2][row] * __builtin_amdgcn_exp2f(m2 - low) +
-                        ls[3][row] * __builtin_amdgcn_exp2f(m3 - low);
-      float x[8];
+      float top = -INFINITY, sum = 0.f, x[8];
+#pragma unroll
+      for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
+      const float low = top == -INFINITY ? 0.f : top;
 #pragma unroll
       for (int i = 0; i < 8; ++i) x[i] = 0.f;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
+      for (int k = 0; k < W; ++k) {
+        sum += ls[k][row] * __builtin_amdgcn_exp2f(ms[k][row] - low);
         const f32x4 y0 = *reinterpret_cast<const f32x4*>(osh + (k * M + row) * OP + d), y1 = *reinterpret_cast<const f32x4*>(osh + (k * M + row) * OP + d + 4);
 #pragma unroll
         for (int i = 0; i < 4; ++i) { x[i] += y0[i]; x[4 + i] += y1[i]; }
@@ -340,14 +347,37 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void p
   }
 }
 
-// Tiles that several workgroups did: the workgroup of this kernel that stands at the first cut inside one joins its parts, 256 values of it, in the
-// order of the keys; its wavefronts take every fourth part.
-template <typename T, int D, int NT> __global__ __launch_bounds__(256) void paged_few_join_kernel(const PagedArgs a) {
-  constexpr int M = 16 * NT;
+// The parts of a tile: running maximum, sum and 4 results of a thread, N parts requested at a time.
+struct FewSum { float m, l; f32x4 o; };
+__device__ __forceinline__ void few_add(FewSum& s, float m, float l, f32x4 o) {
+  const float top = fmaxf(s.m, m), low = top == -INFINITY ? 0.f : top;
+  const float f = __builtin_amdgcn_exp2f(s.m - low), h = __builtin_amdgcn_exp2f(m - low);
+#pragma unroll
+  for (int j = 0; j < 4; ++j) s.o[j] = s.o[j] * f + o[j] * h;
+  s.l = s.l * f + l * h;
+  s.m = top;
+}
+template <int N, int M, int D, class Part> __device__ __forceinline__ void few_add_parts(FewSum& s, int first, int step, Part part, int row, int e) {
+  float m[N], l[N];
+  f32x4 o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float* x = part(first + i * step);
+    m[i] = x[M * D + row]; l[i] = x[M * D + M + row];
+    o[i] = *reinterpret_cast<const f32x4*>(x + e);
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) few_add(s, m[i], l[i], o[i]);
+}
+
+// Tiles that several workgroups did: the workgroup of this kernel that stands at the first cut inside one joins its parts, in the order of
+// the keys.  A wavefront has 256 values of it; up to 16 wavefronts, which take turns with the parts where the values are fewer.
+template <int D, int NT> struct FewJoin { static constexpr int kRuns = 16 * NT * D / 256, kTurns = kRuns > 8 ? 1 : 16 / kRuns, kThreads = 64 * kRuns * kTurns; };
+template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT>::kThreads)) void paged_few_join_kernel(const PagedArgs a) {
+  constexpr int M = 16 * NT, R = FewJoin<D, NT>::kRuns, W = FewJoin<D, NT>::kTurns;
   constexpr int64_t kFloats = FewPart<D, NT>::kFloats;
-  __shared__ float ms[4][64], ls[4][64];
-  __shared__ f32x4 os[4][64];
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  __shared__ FewSum sums[R * W][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), w = wave / R, run = wave - w * R;
   FewLine<NT> line(a);
   line.count();
   const int log_groups = line.groups(), p = blockIdx.x + 1;
@@ -359,57 +389,38 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(256) void page
   if (at == first || before > first) return;      // no part before the cut, or another cut is the first
   int last = p;                                   // the workgroup that the last part is of
   while (line.cut(last + 1, log_groups) < end) ++last;
-  const int e = blockIdx.y * 256 + lane * 4, row = e / D;
+  const int e = run * 256 + lane * 4, row = e / D;
   const int n = last - p + 2;
   auto part = [&](int k) { return a.partial + (2 * (p - 1 + k) + (k == 0 && before != first ? 1 : 0)) * kFloats; };
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = w; k0 < n; k0 += 32) {
-    float pm[8], pl[8];
-    f32x4 po[8];
+  FewSum s{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+  int k = w;
+  for (; k + 7 * W < n; k += 8 * W) few_add_parts<8, M, D>(s, k, W, part, row, e);
+  if (k + 3 * W < n) { few_add_parts<4, M, D>(s, k, W, part, row, e); k += 4 * W; }
+  if (k + W < n) { few_add_parts<2, M, D>(s, k, W, part, row, e); k += 2 * W; }
+  if (k < n) few_add_parts<1, M, D>(s, k, W, part, row, e);
+  if constexpr (W > 1) {
+    sums[wave][lane] = s;
+    __syncthreads();
+    if (w) return;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const float* x = part(min(k0 + 4 * i, n - 1));
-      pm[i] = x[M * D + row]; pl[i] = x[M * D + M + row];
-      po[i] = *reinterpret_cast<const f32x4*>(x + e);
+    for (int i = 1; i < W; ++i) {
+      const FewSum& x = sums[i * R + run][lane];
+      few_add(s, x.m, x.l, x.o);
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (k0 + 4 * i >= n) continue;
-      const float top = fmaxf(m, pm[i]), low = top == -INFINITY ? 0.f : top;
-      const float f = __builtin_amdgcn_exp2f(m - low), h = __builtin_amdgcn_exp2f(pm[i] - low);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = o[j] * f + po[i][j] * h;
-      l = l * f + pl[i] * h;
-      m = top;
-    }
-  }
-  ms[w][lane] = m; ls[w][lane] = l; os[w][lane] = o;
-  __syncthreads();
-  if (w) return;
-  const float top = fmaxf(fmaxf(ms[0][lane], ms[1][lane]), fmaxf(ms[2][lane], ms[3][lane])), low = top == -INFINITY ? 0.f : top;
-  o = f32x4{0.f, 0.f, 0.f, 0.f};
-  l = 0.f;
-#pragma unroll
-  for (int k = 0; k < 4; ++k) {
-    const float h = __builtin_amdgcn_exp2f(ms[k][lane] - low);
-    l += ls[k][lane] * h;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) o[j] += os[k][lane][j] * h;
   }
   if (tile.row0 + row >= tile.r.fresh * a.share) return;
   const int token = (tile.row0 + row) / a.share, head = tile.head * a.share + (tile.row0 + row) - token * a.share;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
+  const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
   *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(tile.r.first + token) * a.out_stride + (int64_t)head * D + e % D) =
-      u32x2{Mfma<T>::pack(o[0] * inv, o[1] * inv), Mfma<T>::pack(o[2] * inv, o[3] * inv)};
-  if (a.lse && e % D == 0) a.lse[(int64_t)(tile.r.first + token) * a.q_heads + head] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+      u32x2{Mfma<T>::pack(s.o[0] * inv, s.o[1] * inv), Mfma<T>::pack(s.o[2] * inv, s.o[3] * inv)};
+  if (a.lse && e % D == 0) a.lse[(int64_t)(tile.r.first + token) * a.q_heads + head] = s.l == 0.f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((paged_few_kernel<T, D, NT>), dim3(1 << a.log_groups), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((paged_few_kernel<T, D, NT>), dim3(a.few_grid), dim3(64 * kFewWaves), 0, s, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3((1 << a.log_groups) - 1, 16 * NT * D / 256), dim3(256), 0, s, a);
+  if (e != hipSuccess || a.log_groups < 0) return e;
+  hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3(a.few_grid - 1), dim3(FewJoin<D, NT>::kThreads), 0, s, a);
   return hipGetLastError();
 }
 

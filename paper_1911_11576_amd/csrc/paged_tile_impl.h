@@ -19,52 +19,150 @@ template <> __device__ __forceinline__ f32x16 mfma32<bf16_t>(u32x4 a, u32x4 b, f
   return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// 16 bytes a lane from memory straight into LDS: piece I of 64 bytes of a lane's row to the wavefront's 1024 bytes at `lds` + 1024 I.
-// (The instruction's offset counts on both sides.  As assembly, since the compiler makes every LDS read behind the builtin wait for
-// all loads in flight, the next step's among them; there is no register that it writes.)
-template <int I> __device__ __forceinline__ void load_lds16(const uint16_t* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory");
-}
-// ... all of them there, before a barrier that hands them on
-__device__ __forceinline__ void wait_lds_loads() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
-__device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) void*)p; }
-
 template <class Op> __device__ __forceinline__ float halves_allreduce(float v) {
   const uint32_t u = as_u32(v);
   const auto r = __builtin_amdgcn_permlane32_swap(u, u, false, false);
   return Op::apply(as_f32(r[0]), as_f32(r[1]));
 }
 
-// Which rows a tile kernel's workgroup has: tile `slot` of the line in which request b's tiles begin at first_b * share / 128 + b (as
-// many places as it can have tiles, whatever the lengths), and which of its keys' parts.
+// What a workgroup of the tile kernel has: a tile of 128 rows, all of its keys or a part of them.
 struct TileWork {
-  int b, row0, rows, key_first, steps, parts, per;      // steps of 64 keys; parts that they are split into, steps of a part
+  int b, head, tile;
   PagedRequest r;
+  int rows, row0, key_first, steps;      // of the request, of the tile: steps of 64 keys
+  int parts, part, partial;              // parts that the keys are split into, this one, and its place among the partial results
 };
-__device__ __forceinline__ bool tile_work(const PagedArgs& a, int slot, TileWork* t) {
-  const int lane = threadIdx.x & 63;
-  auto begin = [&](int b) { return (int)(((int64_t)min(max(a.starts[b], 0), a.tokens) * a.share >> 7)) + b; };
-  int n = 0;
-  for (int b0 = 0; b0 < a.requests; b0 += 64) {
-    const int here = __popcll(__ballot(b0 + lane < a.requests && begin(b0 + lane) <= slot));
-    n += here;
-    if (here < 64) break;
+
+// The order of the work, made by every wavefront for itself from the lengths on the device, up to 64 requests one to a lane.  A tile's
+// time goes with its steps, which differ up to the whole length of the longest request, and workgroups start in order as others end.
+// So: the tiles of more steps than an even share of all (a 512th) are split into parts of at most that and come first; the
+// others follow by falling steps.  Steps do not fall along a request's tiles, so how many of them have at least s is a
+// formula, and the k-th tile is found by bisection over s.  (Chunks of 1 to 1024 tokens behind contexts of up to 12000: the longest tile alone is 1.2
+// times the even share; request by request the launch took 1.48 times it.)
+struct TileLine {
+  const PagedArgs& a;
+  PagedRequest mine{};
+  int tiles = 0, flat = -1;      // of the lane's request; with a window, or without the causal mask: steps of each of its tiles, as good as equal
+  int share_steps = 0;           // an even share
+  int split = 0, parts = 1;      // the lane's tiles of more steps than that (its last ones), and the parts of each
+  int items = 0;                 // parts of all
+
+  __device__ __forceinline__ explicit TileLine(const PagedArgs& args) : a(args) {}
+  static __device__ __forceinline__ int sum(int v) {
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
+    return __builtin_amdgcn_readfirstlane(v);
   }
-  if (n == 0) return false;
-  t->b = n - 1;
-  t->r = paged_request(a, t->b);
-  t->rows = t->r.fresh * a.share;
-  t->row0 = (slot - begin(t->b)) * 128;
-  if (t->rows <= a.few_rows || t->row0 >= t->rows) return false;
-  const int t1 = (min(t->row0 + 128, t->rows) - 1) / a.share, t0 = t->row0 / a.share, back = t->r.keys - t->r.fresh + 1;
-  const int until = max(0, a.causal ? min(t->r.keys, back + t1) : t->r.keys);
-  t->key_first = a.window ? min(max(0, back + t0 - a.window), until) & ~63 : 0;
-  t->steps = (until - t->key_first + 63) / 64;
-  t->parts = min(a.most_parts, max(1, t->steps / a.least_steps));
-  t->per = (t->steps + t->parts - 1) / t->parts;
-  t->parts = t->per ? (t->steps + t->per - 1) / t->per : 1;
-  return true;
-}
+  __device__ __forceinline__ void take(int b) {
+    mine = b < a.requests ? paged_request(a, b) : PagedRequest{};
+    const int rows = mine.fresh * a.share;
+    tiles = rows > a.few_rows ? (rows + 127) >> 7 : 0;
+    flat = -1;
+    if (!a.causal) flat = (mine.keys + 63) >> 6;
+    else if (a.window && a.window < mine.keys) flat = (int)(((int64_t)a.window + 126 + 128 / a.share) >> 6);
+  }
+  // tiles of the lane's request with at least s steps: a tile's last token t has ceil((keys - fresh + 1 + t) / 64)
+  __device__ __forceinline__ int at_least(int s) const {
+    if (s <= 0) return tiles;
+    if (flat >= 0) return flat >= s ? tiles : 0;
+    const int64_t token = 64ll * (s - 1) - (mine.keys - mine.fresh), row = max(token, (int64_t)0) * a.share;      // the first such token, and its first row
+    return row >= (int64_t)mine.fresh * a.share ? 0 : max(0, tiles - (int)(row >> 7));
+  }
+  __device__ __forceinline__ int last_steps() const { return tiles == 0 ? 0 : flat >= 0 ? flat : (mine.keys + 63) >> 6; }
+  __device__ __forceinline__ void order() {
+    take(threadIdx.x & 63);
+    const int last = last_steps(), first = flat >= 0 || tiles == 0 ? last : max(0, mine.keys - mine.fresh + 64) >> 6;
+    // (in 64 steps: no more than 2^31 of them)
+    const int total = sum((int)min((int64_t)tiles * (first + last) * a.kv_heads >> 7, (int64_t)1 << 24));
+    share_steps = max(a.least_steps, total / (kTileShares / 64));
+    for (;; share_steps *= 2) {      // (never more parts than there is room for)
+      split = at_least(share_steps + 1);
+      parts = split ? (last + share_steps - 1) / share_steps : 1;
+      items = sum((int)min((int64_t)split * parts * a.kv_heads, (int64_t)1 << 24));
+      if (items <= 2 * kTileShares) return;
+    }
+  }
+  // the lane among whose `count` the number k falls, k counted from there on
+  static __device__ __forceinline__ int among(int count, int* k) {
+    int upto = count;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const int t = __shfl_up(upto, d);
+      if ((int)(threadIdx.x & 63) >= d) upto += t;
+    }
+    const int lane = min(63, (int)__popcll(__ballot(upto <= *k)));
+    *k -= __builtin_amdgcn_readlane(upto, lane) - __builtin_amdgcn_readlane(count, lane);
+    return lane;
+  }
+  __device__ __forceinline__ void fill(TileWork* t, int lane, int b) const {
+    t->b = b;
+    t->r = PagedRequest{__builtin_amdgcn_readlane(mine.first, lane), __builtin_amdgcn_readlane(mine.fresh, lane), __builtin_amdgcn_readlane(mine.keys, lane)};
+    t->rows = t->r.fresh * a.share;
+    t->row0 = t->tile * 128;
+    const int t1 = (min(t->row0 + 128, t->rows) - 1) / a.share, t0 = t->row0 / a.share, back = t->r.keys - t->r.fresh + 1;
+    const int until = max(0, a.causal ? min(t->r.keys, back + t1) : t->r.keys);
+    t->key_first = a.window ? min(max(0, back + t0 - a.window), until) & ~63 : 0;
+    t->steps = (until - t->key_first + 63) >> 6;
+  }
+  // part k of the split tiles; `whole`: the k-th split tile instead, all of its parts
+  __device__ __forceinline__ void find_split(int k, bool whole, TileWork* t) const {
+    const int per = whole ? split * a.kv_heads : split * a.kv_heads * parts;
+    int in = k;
+    const int lane = among(per, &in);
+    const int n = __builtin_amdgcn_readlane(split, lane) * a.kv_heads;      // tiles and heads of the request
+    t->parts = __builtin_amdgcn_readlane(parts, lane);
+    t->part = whole ? 0 : in / n;
+    const int at = in - t->part * n;
+    t->head = at % a.kv_heads;
+    t->tile = __builtin_amdgcn_readlane(tiles, lane) - __builtin_amdgcn_readlane(split, lane) + at / a.kv_heads;
+    int before = 0;      // parts of the requests before
+    if (whole) {
+      const int all = split * a.kv_heads * parts;
+      before = sum((int)(threadIdx.x & 63) < lane ? all : 0);
+    }
+    t->partial = whole ? before + at : k;
+    fill(t, lane, lane);
+  }
+  // the places of a tile's parts among the partial results are so far apart
+  __device__ __forceinline__ int stride(const TileWork& t) const { return __builtin_amdgcn_readlane(split, t.b) * a.kv_heads; }
+  // the k-th of the tiles that are not split, by falling steps; false: there are not so many
+  __device__ __forceinline__ bool find_whole(int k, TileWork* t) const {
+    if (k >= sum(tiles - split) * a.kv_heads) return false;
+    int lo = 0, hi = share_steps + 1;      // more than k of at least lo steps, no more than k of at least hi
+    while (hi - lo > 1) {
+      const int mid = (lo + hi) >> 1;
+      if (sum(at_least(mid) - split) * a.kv_heads > k) lo = mid; else hi = mid;
+    }
+    const int more = at_least(hi) - split, here = at_least(lo) - split - more;
+    k -= sum(more) * a.kv_heads;
+    const int lane = among(here * a.kv_heads, &k);
+    t->parts = 1; t->part = 0; t->partial = 0;
+    t->head = k % a.kv_heads;
+    t->tile = __builtin_amdgcn_readlane(tiles - split - more - here, lane) + k / a.kv_heads;
+    fill(t, lane, lane);
+    return true;
+  }
+  // more than 64 requests: their tiles in the order of the rows, no one split.  Request b's begin at place first * share / 128 + b (there are
+  // as many places as it can have tiles, whatever the lengths).
+  __device__ __forceinline__ bool find_in_order(int k, TileWork* t) {
+    const int lane = threadIdx.x & 63, slot = a.slots - 1 - k / a.kv_heads;
+    auto begin = [&](int b) { return (int)((int64_t)min(max(a.starts[b], 0), a.tokens) * a.share >> 7) + b; };
+    int n = 0;
+    for (int b0 = 0; b0 < a.requests; b0 += 64) {
+      const int here = __popcll(__ballot(b0 + lane < a.requests && begin(b0 + lane) <= slot));
+      n += here;
+      if (here < 64) break;
+    }
+    if (n == 0) return false;
+    take(n - 1);      // (the same in all lanes)
+    t->tile = slot - begin(n - 1);
+    if (t->tile >= __builtin_amdgcn_readfirstlane(tiles)) return false;
+    t->parts = 1; t->part = 0; t->partial = 0;
+    t->head = k % a.kv_heads;
+    fill(t, 0, n - 1);
+    return true;
+  }
+};
 
 // 64 keys (or values) in LDS as the direct loads leave them: 16 keys to a wavefront's part, pieces of 64 bytes of them behind one
 // another, [key / 16][64-byte piece][key % 16][4 x 16 bytes].  The 16 bytes x of a piece of key r stand in place x ^ (r / 4 % 4): eight lanes that
@@ -80,12 +178,21 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
   __shared__ uint32_t flags[2][4], odds[4];                 // which of a wavefront's 16 keys are there; whether a value of them is infinite or NaN
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
-  const int head = blockIdx.x % a.kv_heads, rest = blockIdx.x / a.kv_heads;
-  const int part = rest % a.most_parts, slot = a.slots - 1 - rest / a.most_parts;      // the last tiles of a request have the most keys: first
   TileWork work;
-  if (!tile_work(a, slot, &work) || part >= work.parts) return;
+  {
+    TileLine line(a);
+    if (a.requests > 64) {
+      if (!line.find_in_order(blockIdx.x, &work)) return;
+    } else {
+      line.order();
+      if ((int)blockIdx.x < line.items) line.find_split(blockIdx.x, false, &work);
+      else if (!line.find_whole(blockIdx.x - line.items, &work)) return;
+    }
+  }
   const PagedRequest r = work.r;
-  const int step0 = part * work.per, steps = min(work.per, work.steps - step0);
+  const int head = work.head;
+  // a part's steps: an even run of the tile's
+  const int step0 = (int)((int64_t)work.steps * work.part / work.parts), steps = (int)((int64_t)work.steps * (work.part + 1) / work.parts) - step0;
   const int key_first = work.key_first + 64 * step0;
   const int* table = a.tables + (int64_t)work.b * a.width;
   const int in_block = (1 << a.cache.shift) - 1;
@@ -137,11 +244,11 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
     const bool ok = key < key_last && (unsigned)block < (unsigned)a.cache.blocks;
     const int64_t at = (int64_t)(ok ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot;
     const uint32_t kl = lds_address(&ksh[buf].v[w * K16]), vl = lds_address(&vsh[buf].v[w * K16]);
-    load_lds16<0>(kbase + at, kl);
-    load_lds16<0>(vbase + at, vl);
-    if constexpr (CH > 1) { load_lds16<1>(kbase + at, kl); load_lds16<1>(vbase + at, vl); }
-    if constexpr (CH > 2) { load_lds16<2>(kbase + at, kl); load_lds16<2>(vbase + at, vl); }
-    if constexpr (CH > 3) { load_lds16<3>(kbase + at, kl); load_lds16<3>(vbase + at, vl); }
+    load_lds16<0, false>(kbase + at, kl);
+    load_lds16<0, false>(vbase + at, vl);
+    if constexpr (CH > 1) { load_lds16<1, false>(kbase + at, kl); load_lds16<1, false>(vbase + at, vl); }
+    if constexpr (CH > 2) { load_lds16<2, false>(kbase + at, kl); load_lds16<2, false>(vbase + at, vl); }
+    if constexpr (CH > 3) { load_lds16<3, false>(kbase + at, kl); load_lds16<3, false>(vbase + at, vl); }
     const uint64_t good = __ballot(ok);
     uint32_t flag = 0xffffu;
     if (good != ~0ull) {
@@ -272,7 +379,7 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
     request_block(key_first);
     request_rows(key_first, 0);
     request_block(key_first + 64);
-    wait_lds_loads();
+    wait_loads<0>();
     __syncthreads();
     for (int i = 0; i < steps; ++i) {
       const int key0 = key_first + 64 * i;
@@ -281,14 +388,14 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
         request_block(key0 + 128);
       }
       compute(key0, i & 1);
-      wait_lds_loads();
+      wait_loads<0>();
       __syncthreads();
     }
   }
   l = halves_allreduce<SumOp>(l);
   const float top = m == -INFINITY ? -INFINITY : m * scale2;      // in units of log 2
   if (work.parts > 1) {
-    float* at = a.tile_partial + ((int64_t)(slot * a.kv_heads + head) * a.most_parts + part) * (128 * (D + 2));
+    float* at = a.tile_partial + (int64_t)work.partial * (128 * (D + 2));
     const int mine = 32 * w + c;
 #pragma unroll
     for (int dt = 0; dt < DT; ++dt)
@@ -310,48 +417,55 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
   if (a.lse && h == 0) a.lse[(int64_t)(r.first + token) * a.q_heads + q_head] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// 1024 values of a tile whose keys were split, four to a thread: the parts in the order of the keys.
+// 4096 values of a tile whose keys were split, sixteen to a thread: the parts in the order of the keys.
 template <typename T, int D> __global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a) {
-  const int head = blockIdx.x % a.kv_heads, slot = blockIdx.x / a.kv_heads;
+  TileLine line(a);
+  line.order();
+  if ((int)blockIdx.x >= TileLine::sum(line.split) * a.kv_heads) return;
   TileWork work;
-  if (!tile_work(a, slot, &work) || work.parts == 1) return;
-  const int e = (blockIdx.y * 256 + threadIdx.x) * 4, mine = e / D, row = work.row0 + mine;
-  if (row >= work.rows) return;
-  const float* at = a.tile_partial + (int64_t)(slot * a.kv_heads + head) * a.most_parts * (128 * (D + 2));
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
-  for (int k0 = 0; k0 < work.parts; k0 += 4) {
-    float pm[4], pl[4];
-    f32x4 po[4];
+  line.find_split(blockIdx.x, true, &work);
+  const int64_t stride = (int64_t)line.stride(work) * (128 * (D + 2));
+  const float* at = a.tile_partial + (int64_t)work.partial * (128 * (D + 2));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float* x = at + (int64_t)min(k0 + i, work.parts - 1) * (128 * (D + 2));
-      pm[i] = x[128 * D + mine]; pl[i] = x[128 * D + 128 + mine];
-      po[i] = *reinterpret_cast<const f32x4*>(x + e);
+  for (int j = 0; j < 4; ++j) {
+    const int e = (blockIdx.y * 1024 + j * 256 + threadIdx.x) * 4, mine = e / D, row = work.row0 + mine;
+    if (row >= work.rows) continue;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int k0 = 0; k0 < work.parts; k0 += 4) {
+      float pm[4], pl[4];
+      f32x4 po[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float* x = at + min(k0 + i, work.parts - 1) * stride;
+        pm[i] = x[128 * D + mine]; pl[i] = x[128 * D + 128 + mine];
+        po[i] = *reinterpret_cast<const f32x4*>(x + e);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (k0 + i >= work.parts) continue;
+        const float top = fmaxf(m, pm[i]), low = top == -INFINITY ? 0.f : top;
+        const float f = __builtin_amdgcn_exp2f(m - low), g = __builtin_amdgcn_exp2f(pm[i] - low);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) o[q] = o[q] * f + po[i][q] * g;
+        l = l * f + pl[i] * g;
+        m = top;
+      }
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (k0 + i >= work.parts) continue;
-      const float top = fmaxf(m, pm[i]), low = top == -INFINITY ? 0.f : top;
-      const float f = __builtin_amdgcn_exp2f(m - low), g = __builtin_amdgcn_exp2f(pm[i] - low);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[j] = o[j] * f + po[i][j] * g;
-      l = l * f + pl[i] * g;
-      m = top;
-    }
+    const int token = row / a.share, q_head = work.head * a.share + row - token * a.share;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(work.r.first + token) * a.out_stride + (int64_t)q_head * D + e % D) =
+        u32x2{Mfma<T>::pack(o[0] * inv, o[1] * inv), Mfma<T>::pack(o[2] * inv, o[3] * inv)};
+    if (a.lse && e % D == 0) a.lse[(int64_t)(work.r.first + token) * a.q_heads + q_head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
-  const int token = row / a.share, q_head = head * a.share + row - token * a.share;
-  const float inv = l == 0.f ? 0.f : 1.f / l;
-  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(work.r.first + token) * a.out_stride + (int64_t)q_head * D + e % D) =
-      u32x2{Mfma<T>::pack(o[0] * inv, o[1] * inv), Mfma<T>::pack(o[2] * inv, o[3] * inv)};
-  if (a.lse && e % D == 0) a.lse[(int64_t)(work.r.first + token) * a.q_heads + q_head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
 template <typename T, int D> hipError_t paged_tile_launch(const PagedArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((paged_tile_kernel<T, D>), dim3((unsigned)(a.slots * a.kv_heads * a.most_parts)), dim3(256), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.most_parts == 1) return e;
-  hipLaunchKernelGGL((paged_tile_join_kernel<T, D>), dim3((unsigned)(a.slots * a.kv_heads), D / 8), dim3(256), 0, s, a);
+  const bool ordered = a.requests <= 64;
+  hipLaunchKernelGGL((paged_tile_kernel<T, D>), dim3((unsigned)(a.slots * a.kv_heads + (ordered ? 2 * kTileShares : 0))), dim3(256), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || !ordered) return e;
+  hipLaunchKernelGGL((paged_tile_join_kernel<T, D>), dim3(kTileShares, D / 32), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
