@@ -15,43 +15,41 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   s->row_tiles = (many ? s->share : rows) <= 16 ? 1 : 2;
   s->few_rows = many ? 16 * s->row_tiles : 1 << 30;
   const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;      // at most
-  const int64_t m = 16 * s->row_tiles;
-  s->few_bytes = 0;
-  if (keys <= 1024 && tiles <= 65536) {
+  const int64_t m = 16 * s->row_tiles, waves = many ? 4 : 8;
+  const bool any = d.tokens && d.requests;
+  if (!many && keys <= 1024 && tiles <= 65536) {
     // no request is longer than four steps: a workgroup each tile, nothing to join
     s->log_groups = -1;
     s->unit_keys = 1024;
     s->few_grid = (int)tiles;
   } else {
-    s->log_groups = 8;
+    // as many wavefronts as the chip holds, eight to a CU
+    s->log_groups = many ? 9 : 8;
     s->few_grid = 1 << s->log_groups;
-    s->unit_keys = 256;
+    s->unit_keys = 32 * (int)waves;
     // units are numbered in 31 bits
     while (tiles * (keys / s->unit_keys + 1) > 0x7fffffffll) {
       if (s->unit_keys >= (1 << 29)) { *err = "too many rows"; return false; }
       s->unit_keys *= 2;
     }
-    if (d.tokens && d.requests) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
+    if (any) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
   }
   s->partial_bytes = s->few_bytes;
   *n_kernels = s->log_groups < 0 ? 1 : 2;
-  const int64_t pad = d.head_dim == 64 ? 8 : 16;
-  *lds_bytes = std::max<int64_t>(8 * 32 * (d.head_dim + pad) * 2, 8 * m * (d.head_dim + 4) * 4) + 64 * m;
-  s->slots = 0;
+  *lds_bytes = std::max<int64_t>(waves * 128 * d.head_dim, waves * m * (d.head_dim + 4) * 4) + waves * (512 + 8 * m);
   if (many) {
     s->slots = ((int64_t)d.tokens * s->share >> 7) + d.requests;
-    if (s->slots * d.kv_heads > 0x7ffffbffll) { *err = "too many tiles for one grid"; return false; }
-    const bool ordered = d.requests <= 64;
-    if (ordered && d.tokens && d.requests) s->partial_bytes += 2ll * kTileShares * 128 * (d.head_dim + 2) * 4;
-    *n_kernels += ordered ? 2 : 1;
-    *lds_bytes = std::max<int64_t>(*lds_bytes, 2ll * 64 * 2 * 2 * d.head_dim + 48);
+    if (s->slots * d.kv_heads > 0x7ffff000ll) { *err = "too many tiles for one grid"; return false; }
+    if (any && d.requests <= 64) s->partial_bytes += 2ll * kTileShares * 128 * (d.head_dim + 2) * 4;
+    *lds_bytes = std::max<int64_t>(*lds_bytes, 512 * d.head_dim + 48);
   }
   return true;
 }
 
 std::string paged_attn_describe(const PagedAttnSpec& s) {
   char buf[320];
-  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=512%s", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.log_groups < 0 ? "" : "; join[GRID,CTA]");
+  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=%d%s", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.slots ? 256 : 512,
+                   s.log_groups < 0 ? "" : "; join[GRID,CTA]");
   if (s.slots) snprintf(buf + n, sizeof buf - n, "; requests of more than %d rows: rows to a tile=128, cta_num=%lld", s.few_rows, (long long)(s.slots * s.d.kv_heads));
   return buf;
 }
@@ -76,9 +74,8 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;
   a.slots = (int)s.slots; a.least_steps = s.least_steps;
   const bool f16 = s.d.dtype == FS_F16;
-  hipError_t e = hipSuccess;
-  if (s.slots) e = (f16 ? paged_tile_launch_f16 : paged_tile_launch_bf16)(a, s.d.head_dim, st);
-  if (e == hipSuccess) e = (f16 ? paged_few_launch_f16 : paged_few_launch_bf16)(a, s.d.head_dim, s.row_tiles, st);
+  const hipError_t e = s.slots ? (f16 ? paged_mixed_launch_f16 : paged_mixed_launch_bf16)(a, s.d.head_dim, s.row_tiles, st)
+                               : (f16 ? paged_few_launch_f16 : paged_few_launch_bf16)(a, s.d.head_dim, s.row_tiles, st);
   if (e != hipSuccess) { *err = std::string("paged_attention launch: ") + hipGetErrorString(e); return -1; }
   return 0;
 }

@@ -46,6 +46,28 @@ __device__ __forceinline__ int paged_first_key(const PagedArgs& a, const PagedRe
   return a.window ? max(0, r.keys - r.fresh + 1 - a.window) & ~31 : 0;
 }
 
+// Sum over the wavefront's lanes, the same in all of them.
+__device__ __forceinline__ int wave_sum(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false);
+  auto r = __builtin_amdgcn_permlane16_swap((uint32_t)v, (uint32_t)v, false, false);
+  v = (int)(r[0] + r[1]);
+  r = __builtin_amdgcn_permlane32_swap((uint32_t)v, (uint32_t)v, false, false);
+  return __builtin_amdgcn_readfirstlane((int)(r[0] + r[1]));
+}
+// Sum over the lanes up to and with this one: inside rows of 16 by shifts, then the last lane of the row before, and of the half before.
+__device__ __forceinline__ int wave_upto(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);
+  return v;
+}
+
 // Values of a 16-byte piece that are infinite or NaN: the exponent's bits are all ones, which the addition carries into the sign's place.
 template <typename T> struct Odd;
 template <> struct Odd<f16_t> { static constexpr uint32_t kMask = 0x7c007c00u, kCarry = 0x04000400u; };
@@ -87,8 +109,8 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_
 // few rows a request: the work split evenly over a fixed grid, then the parts joined
 hipError_t paged_few_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 hipError_t paged_few_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
-// many rows a request: tiles of 128
-hipError_t paged_tile_launch_f16(const PagedArgs&, int dim, hipStream_t);
-hipError_t paged_tile_launch_bf16(const PagedArgs&, int dim, hipStream_t);
+// many rows a request, in tiles of 128, and few rows, in one
+hipError_t paged_mixed_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged_mixed_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 
 }  // namespace fs

@@ -40,12 +40,7 @@ template <int NT> struct FewLine {
       mine = paged_request(a, b);
       if (mine.fresh * a.share <= a.few_rows) units = (uint32_t)((mine.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(mine) * (uint32_t)a.kv_heads;
     }
-    upto = units;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t t = __shfl_up(upto, d);
-      if ((int)(threadIdx.x & 63) >= d) upto += t;
-    }
+    upto = (uint32_t)wave_upto((int)units);
     all = __builtin_amdgcn_readlane(upto, 63);
   }
   __device__ __forceinline__ void count() {
@@ -88,22 +83,32 @@ template <int NT> struct FewLine {
 // same 16 bytes of eight rows, and the four rows of a transposing read, fall on different banks.
 template <int D> __device__ __forceinline__ int few_turn(int row) { return D == 128 ? 2 * (row & 7) : D == 64 ? row & 6 : row >> 1 & 2; }
 
-template <typename T, int D, int NT> __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(const PagedArgs a) {
-  constexpr int W = kFewWaves, KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 32 * W, C = D / 8, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 32 rows
-  constexpr int OP = D + 4;                        // row of results in LDS (floats)
-  constexpr int kLds = W * 64 * D * 2 > W * M * OP * 4 ? W * 64 * D * 2 : W * M * OP * 4;
-  __shared__ __align__(1024) unsigned char smem[kLds];
-  __shared__ int blocks[W][2][64];                 // block numbers of the keys to come
-  __shared__ float ms[W][M], ls[W][M];
+// LDS of a workgroup of W wavefronts: keys and values of each while it reads them, then results.
+template <int D, int NT, int W> struct FewLds {
+  static constexpr int M = 16 * NT, OP = D + 4;      // OP: row of results (floats)
+  union {
+    uint16_t rows[W][2][32 * D];
+    float results[W][M * OP];
+  };
+  int blocks[W][2][64];                              // block numbers of the keys to come
+  float ms[W][M], ls[W][M];
+};
+
+// Workgroup p of 1 << log_groups (of as many as there are tiles where log_groups is -1).
+template <typename T, int D, int NT, int W> __device__ __forceinline__ void paged_few(const PagedArgs& a, FewLds<D, NT, W>& lds, int p) {
+  constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 32 * W, C = D / 8, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 32 rows
+  constexpr int OP = FewLds<D, NT, W>::OP;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int c = lane & 15, g = lane >> 4;
-  uint16_t *ksh = reinterpret_cast<uint16_t*>(smem) + w * 64 * D, *vsh = ksh + 32 * D;
-  const uint32_t k_lds = lds_address(ksh), v_lds = lds_address(vsh), b_lds = lds_address(&blocks[w][0][0]);
-  float* osh = reinterpret_cast<float*>(smem);
+  uint16_t *ksh = lds.rows[w][0], *vsh = lds.rows[w][1];
+  const uint32_t k_lds = lds_address(ksh), v_lds = lds_address(vsh), b_lds = lds_address(&lds.blocks[w][0][0]);
+  float* osh = &lds.results[0][0];
+  auto& blocks = lds.blocks;
+  auto& ms = lds.ms;
+  auto& ls = lds.ls;
 
   FewLine<NT> line(a);
   line.count();
-  const int p = blockIdx.x;
   uint32_t u0, u1;
   if (a.log_groups < 0) {      // a unit is a tile, a workgroup has one
     u0 = p; u1 = p + 1;
@@ -347,6 +352,11 @@ template <typename T, int D, int NT> __global__ __launch_bounds__(64 * kFewWaves
   }
 }
 
+template <typename T, int D, int NT> __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(const PagedArgs a) {
+  __shared__ __align__(1024) FewLds<D, NT, kFewWaves> lds;
+  paged_few<T, D, NT, kFewWaves>(a, lds, blockIdx.x);
+}
+
 // The parts of a tile: running maximum, sum and 4 results of a thread, N parts requested at a time.
 struct FewSum { float m, l; f32x4 o; };
 __device__ __forceinline__ void few_add(FewSum& s, float m, float l, f32x4 o) {
@@ -370,17 +380,17 @@ template <int N, int M, int D, class Part> __device__ __forceinline__ void few_a
   for (int i = 0; i < N; ++i) few_add(s, m[i], l[i], o[i]);
 }
 
-// Tiles that several workgroups did: the workgroup of this kernel that stands at the first cut inside one joins its parts, in the order of
+// Tiles that several workgroups did: the workgroup that stands at the first cut p inside one joins its parts, in the order of
 // the keys.  A wavefront has 256 values of it; up to 16 wavefronts, which take turns with the parts where the values are fewer.
 template <int D, int NT> struct FewJoin { static constexpr int kRuns = 16 * NT * D / 256, kTurns = kRuns > 8 ? 1 : 16 / kRuns, kThreads = 64 * kRuns * kTurns; };
-template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT>::kThreads)) void paged_few_join_kernel(const PagedArgs a) {
+template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_join(const PagedArgs& a, int p) {
   constexpr int M = 16 * NT, R = FewJoin<D, NT>::kRuns, W = FewJoin<D, NT>::kTurns;
   constexpr int64_t kFloats = FewPart<D, NT>::kFloats;
   __shared__ FewSum sums[R * W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), w = wave / R, run = wave - w * R;
   FewLine<NT> line(a);
   line.count();
-  const int log_groups = line.groups(), p = blockIdx.x + 1;
+  const int log_groups = line.groups();
   if (p >> log_groups) return;
   const uint32_t at = line.cut(p, log_groups);
   if (at >= line.total) return;
@@ -414,6 +424,10 @@ template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT
   *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(tile.r.first + token) * a.out_stride + (int64_t)head * D + e % D) =
       u32x2{Mfma<T>::pack(s.o[0] * inv, s.o[1] * inv), Mfma<T>::pack(s.o[2] * inv, s.o[3] * inv)};
   if (a.lse && e % D == 0) a.lse[(int64_t)(tile.r.first + token) * a.q_heads + head] = s.l == 0.f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * 0.6931471805599453f;
+}
+
+template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT>::kThreads)) void paged_few_join_kernel(const PagedArgs a) {
+  paged_few_join<T, D, NT>(a, blockIdx.x + 1);
 }
 
 template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs& a, hipStream_t s) {

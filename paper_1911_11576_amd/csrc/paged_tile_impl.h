@@ -5,7 +5,9 @@
 // barrier a step.  Both dots are v_mfma_f32_32x32x16.  Where there are few tiles their keys are split over workgroups too, and
 // paged_tile_join_kernel adds the parts in the order of the keys.
 #pragma once
-#include "paged_attn_impl.h"
+#include <algorithm>
+
+#include "paged_few_impl.h"
 
 namespace fs {
 
@@ -48,11 +50,6 @@ struct TileLine {
   int items = 0;                 // parts of all
 
   __device__ __forceinline__ explicit TileLine(const PagedArgs& args) : a(args) {}
-  static __device__ __forceinline__ int sum(int v) {
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) v += __shfl_xor(v, d);
-    return __builtin_amdgcn_readfirstlane(v);
-  }
   __device__ __forceinline__ void take(int b) {
     mine = b < a.requests ? paged_request(a, b) : PagedRequest{};
     const int rows = mine.fresh * a.share;
@@ -73,23 +70,18 @@ struct TileLine {
     take(threadIdx.x & 63);
     const int last = last_steps(), first = flat >= 0 || tiles == 0 ? last : max(0, mine.keys - mine.fresh + 64) >> 6;
     // (in 64 steps: no more than 2^31 of them)
-    const int total = sum((int)min((int64_t)tiles * (first + last) * a.kv_heads >> 7, (int64_t)1 << 24));
+    const int total = wave_sum((int)min((int64_t)tiles * (first + last) * a.kv_heads >> 7, (int64_t)1 << 24));
     share_steps = max(a.least_steps, total / (kTileShares / 64));
     for (;; share_steps *= 2) {      // (never more parts than there is room for)
       split = at_least(share_steps + 1);
       parts = split ? (last + share_steps - 1) / share_steps : 1;
-      items = sum((int)min((int64_t)split * parts * a.kv_heads, (int64_t)1 << 24));
+      items = wave_sum((int)min((int64_t)split * parts * a.kv_heads, (int64_t)1 << 24));
       if (items <= 2 * kTileShares) return;
     }
   }
   // the lane among whose `count` the number k falls, k counted from there on
   static __device__ __forceinline__ int among(int count, int* k) {
-    int upto = count;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const int t = __shfl_up(upto, d);
-      if ((int)(threadIdx.x & 63) >= d) upto += t;
-    }
+    const int upto = wave_upto(count);
     const int lane = min(63, (int)__popcll(__ballot(upto <= *k)));
     *k -= __builtin_amdgcn_readlane(upto, lane) - __builtin_amdgcn_readlane(count, lane);
     return lane;
@@ -118,7 +110,7 @@ struct TileLine {
     int before = 0;      // parts of the requests before
     if (whole) {
       const int all = split * a.kv_heads * parts;
-      before = sum((int)(threadIdx.x & 63) < lane ? all : 0);
+      before = wave_sum((int)(threadIdx.x & 63) < lane ? all : 0);
     }
     t->partial = whole ? before + at : k;
     fill(t, lane, lane);
@@ -127,14 +119,14 @@ struct TileLine {
   __device__ __forceinline__ int stride(const TileWork& t) const { return __builtin_amdgcn_readlane(split, t.b) * a.kv_heads; }
   // the k-th of the tiles that are not split, by falling steps; false: there are not so many
   __device__ __forceinline__ bool find_whole(int k, TileWork* t) const {
-    if (k >= sum(tiles - split) * a.kv_heads) return false;
+    if (k >= wave_sum(tiles - split) * a.kv_heads) return false;
     int lo = 0, hi = share_steps + 1;      // more than k of at least lo steps, no more than k of at least hi
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (sum(at_least(mid) - split) * a.kv_heads > k) lo = mid; else hi = mid;
+      if (wave_sum(at_least(mid) - split) * a.kv_heads > k) lo = mid; else hi = mid;
     }
     const int more = at_least(hi) - split, here = at_least(lo) - split - more;
-    k -= sum(more) * a.kv_heads;
+    k -= wave_sum(more) * a.kv_heads;
     const int lane = among(here * a.kv_heads, &k);
     t->parts = 1; t->part = 0; t->partial = 0;
     t->head = k % a.kv_heads;
@@ -172,21 +164,28 @@ template <int D> struct TileLds {
   uint16_t v[64 * D];
 };
 
-template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_tile_kernel(const PagedArgs a) {
+template <int D> struct TileShared {
+  TileLds<D> k[2], v[2];
+  uint32_t flags[2][4], odds[4];                            // which of a wavefront's 16 keys are there; whether a value of them is infinite or NaN
+};
+
+// Workgroup k of the tile kernel.
+template <typename T, int D> __device__ __forceinline__ void paged_tile(const PagedArgs& a, TileShared<D>& lds, int k) {
   constexpr int KS = D / 16, DT = D / 32, CH = D / 32, K16 = 16 * D;
-  __shared__ __align__(1024) TileLds<D> ksh[2], vsh[2];
-  __shared__ uint32_t flags[2][4], odds[4];                 // which of a wavefront's 16 keys are there; whether a value of them is infinite or NaN
+  auto &ksh = lds.k, &vsh = lds.v;
+  auto& flags = lds.flags;
+  auto& odds = lds.odds;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int c = lane & 31, h = lane >> 5;
   TileWork work;
   {
     TileLine line(a);
     if (a.requests > 64) {
-      if (!line.find_in_order(blockIdx.x, &work)) return;
+      if (!line.find_in_order(k, &work)) return;
     } else {
       line.order();
-      if ((int)blockIdx.x < line.items) line.find_split(blockIdx.x, false, &work);
-      else if (!line.find_whole(blockIdx.x - line.items, &work)) return;
+      if (k < line.items) line.find_split(k, false, &work);
+      else if (!line.find_whole(k - line.items, &work)) return;
     }
   }
   const PagedRequest r = work.r;
@@ -417,64 +416,74 @@ template <typename T, int D> __global__ __launch_bounds__(256, 2) void paged_til
   if (a.lse && h == 0) a.lse[(int64_t)(r.first + token) * a.q_heads + q_head] = l == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
 }
 
-// 4096 values of a tile whose keys were split, sixteen to a thread: the parts in the order of the keys.
-template <typename T, int D> __global__ __launch_bounds__(256) void paged_tile_join_kernel(const PagedArgs a) {
+// Tiles whose keys were split: workgroup b of `groups` joins every groups-th run of 4096 values of them, the parts in the order of the keys.
+template <typename T, int D> __device__ __forceinline__ void paged_tile_join(const PagedArgs& a, int b, int groups) {
   TileLine line(a);
   line.order();
-  if ((int)blockIdx.x >= TileLine::sum(line.split) * a.kv_heads) return;
-  TileWork work;
-  line.find_split(blockIdx.x, true, &work);
-  const int64_t stride = (int64_t)line.stride(work) * (128 * (D + 2));
-  const float* at = a.tile_partial + (int64_t)work.partial * (128 * (D + 2));
-#pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    const int e = (blockIdx.y * 1024 + j * 256 + threadIdx.x) * 4, mine = e / D, row = work.row0 + mine;
-    if (row >= work.rows) continue;
-    float m = -INFINITY, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    for (int k0 = 0; k0 < work.parts; k0 += 4) {
-      float pm[4], pl[4];
-      f32x4 po[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float* x = at + min(k0 + i, work.parts - 1) * stride;
-        pm[i] = x[128 * D + mine]; pl[i] = x[128 * D + 128 + mine];
-        po[i] = *reinterpret_cast<const f32x4*>(x + e);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (k0 + i >= work.parts) continue;
-        const float top = fmaxf(m, pm[i]), low = top == -INFINITY ? 0.f : top;
-        const float f = __builtin_amdgcn_exp2f(m - low), g = __builtin_amdgcn_exp2f(pm[i] - low);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) o[q] = o[q] * f + po[i][q] * g;
-        l = l * f + pl[i] * g;
-        m = top;
-      }
+  const int runs = wave_sum(line.split) * a.kv_heads * (D / 32);
+  for (; b < runs; b += groups) {
+    const int k = b / (D / 32), run = b - k * (D / 32);
+    TileWork work;
+    line.find_split(k, true, &work);
+    const int64_t stride = (int64_t)line.stride(work) * (128 * (D + 2));
+    const float* at = a.tile_partial + (int64_t)work.partial * (128 * (D + 2));
+    for (int i = threadIdx.x; i < 1024; i += blockDim.x) {
+      const int e = (run * 1024 + i) * 4, mine = e / D, row = work.row0 + mine;
+      if (row >= work.rows) continue;
+      FewSum s{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
+      auto part = [&](int n) { return at + n * stride; };
+      int n = 0;
+      for (; n + 4 <= work.parts; n += 4) few_add_parts<4, 128, D>(s, n, 1, part, mine, e);
+      if (n + 2 <= work.parts) { few_add_parts<2, 128, D>(s, n, 1, part, mine, e); n += 2; }
+      if (n < work.parts) few_add_parts<1, 128, D>(s, n, 1, part, mine, e);
+      const int token = row / a.share, q_head = work.head * a.share + row - token * a.share;
+      const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
+      *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(work.r.first + token) * a.out_stride + (int64_t)q_head * D + e % D) =
+          u32x2{Mfma<T>::pack(s.o[0] * inv, s.o[1] * inv), Mfma<T>::pack(s.o[2] * inv, s.o[3] * inv)};
+      if (a.lse && e % D == 0) a.lse[(int64_t)(work.r.first + token) * a.q_heads + q_head] = s.l == 0.f ? -INFINITY : (s.m + __builtin_amdgcn_logf(s.l)) * 0.6931471805599453f;
     }
-    const int token = row / a.share, q_head = work.head * a.share + row - token * a.share;
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(work.r.first + token) * a.out_stride + (int64_t)q_head * D + e % D) =
-        u32x2{Mfma<T>::pack(o[0] * inv, o[1] * inv), Mfma<T>::pack(o[2] * inv, o[3] * inv)};
-    if (a.lse && e % D == 0) a.lse[(int64_t)(work.r.first + token) * a.q_heads + q_head] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
   }
 }
 
-template <typename T, int D> hipError_t paged_tile_launch(const PagedArgs& a, hipStream_t s) {
+// Requests of few rows and of many in one launch, and one that joins the parts of both: the former read memory while the latter keep the
+// matrix unit busy, and where there are none of them (whole prompts) they cost no launches of their own.
+template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(const PagedArgs a) {
+  __shared__ __align__(1024) union { FewLds<D, NT, 4> few; TileShared<D> tile; } lds;
+  const int tiles = gridDim.x - a.few_grid, b = blockIdx.x;
+  if (b < tiles) paged_tile<T, D>(a, lds.tile, b);
+  else paged_few<T, D, NT, 4>(a, lds.few, b - tiles);
+}
+template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT>::kThreads)) void paged_mixed_join_kernel(const PagedArgs a) {
+  // 256 workgroups for either kind: what there is to join is known on the device alone, mostly little
+  if (blockIdx.x >= 256) {
+    paged_tile_join<T, D>(a, blockIdx.x - 256, 256);
+    return;
+  }
+  for (int p = blockIdx.x + 1; p < a.few_grid; p += 256) {
+    paged_few_join<T, D, NT>(a, p);
+    __syncthreads();
+  }
+}
+
+template <typename T, int D, int NT> hipError_t paged_mixed_launch(const PagedArgs& a, hipStream_t s) {
   const bool ordered = a.requests <= 64;
-  hipLaunchKernelGGL((paged_tile_kernel<T, D>), dim3((unsigned)(a.slots * a.kv_heads + (ordered ? 2 * kTileShares : 0))), dim3(256), 0, s, a);
+  const int tiles = std::max(a.few_grid, a.slots * a.kv_heads + (ordered ? 2 * kTileShares : 0));
+  hipLaunchKernelGGL((paged_mixed_kernel<T, D, NT>), dim3((unsigned)(a.few_grid + tiles)), dim3(256), 0, s, a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || !ordered) return e;
-  hipLaunchKernelGGL((paged_tile_join_kernel<T, D>), dim3(kTileShares, D / 32), dim3(256), 0, s, a);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((paged_mixed_join_kernel<T, D, NT>), dim3(ordered ? 512 : 256), dim3(FewJoin<D, NT>::kThreads), 0, s, a);
   return hipGetLastError();
 }
 
-template <typename T> hipError_t paged_tile_launch_type(const PagedArgs& a, int dim, hipStream_t s) {
+template <typename T, int D> hipError_t paged_mixed_launch_rows(const PagedArgs& a, int row_tiles, hipStream_t s) {
+  return row_tiles == 1 ? paged_mixed_launch<T, D, 1>(a, s) : paged_mixed_launch<T, D, 2>(a, s);
+}
+template <typename T> hipError_t paged_mixed_launch_type(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) {
   switch (dim) {
-    case 32: return paged_tile_launch<T, 32>(a, s);
-    case 64: return paged_tile_launch<T, 64>(a, s);
-    case 96: return paged_tile_launch<T, 96>(a, s);
-    default: return paged_tile_launch<T, 128>(a, s);
+    case 32: return paged_mixed_launch_rows<T, 32>(a, row_tiles, s);
+    case 64: return paged_mixed_launch_rows<T, 64>(a, row_tiles, s);
+    case 96: return paged_mixed_launch_rows<T, 96>(a, row_tiles, s);
+    default: return paged_mixed_launch_rows<T, 128>(a, row_tiles, s);
   }
 }
 
