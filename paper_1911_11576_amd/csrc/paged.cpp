@@ -183,7 +183,6 @@ fs_status fs_plan_create_rotary(const fs_rotary_desc* desc, fs_plan** out) {
     s.units = (int)((dim + 2 * w - 1) / (2 * w));
     s.heads = d.q_heads + d.k_heads * (store ? 2 : 1);
     fs::rotary_geometry(&s);
-    if (s.grid > 0x7fffffffll) { *err = "too many rows for one grid"; return false; }
     const int64_t q_row = d.q_heads * dim, k_row = d.k_heads * dim;
     fs::PagedPlan& g = p->paged;
     g.kind = FS_SCHED_ROTARY;
@@ -201,8 +200,8 @@ fs_status fs_plan_create_rotary(const fs_rotary_desc* desc, fs_plan** out) {
       g.out.push_back({"k_out", rows_bytes(t, d.k_out_stride, k_row, e), d.k_stride == d.k_out_stride ? 1 : -1});
     }
     g.bytes = 2 * t * dim * s.heads * e + t * (store ? 8 : 4) + 4ll * d.rotary_dim;
-    p->description = numbers("rotary[GRID-WARP,THREAD] width=%lld, units=%lld, heads_at_once=%lld, rows_per_cta=%lld; cta_num=%lld, cta_size=%lld", s.width, s.units, s.heads_at_once,
-                             s.tokens_per_wg, s.grid, s.wg) + (store ? ", stores k and v in the cache" : "");
+    p->description = numbers("rotary[GRID-WARP,THREAD] width=%lld, units=%lld, heads_each=%lld; cta_num=%lld, cta_size=256", s.width, s.units, s.heads_each,
+                             (t * s.units * s.groups + 255) / 256) + (store ? ", stores k and v in the cache" : "");
     return true;
   });
 }

@@ -19,8 +19,8 @@ struct RotarySpec {
   fs_rotary_desc d{};
   CacheLayout cache;
   int width = 1;                   // elements of a vector
-  int units = 1, heads_at_once = 1, heads = 1, tokens_per_wg = 1, wg = 64;      // threads to a head, heads of a token at a time, heads in all
-  int64_t grid = 1;
+  int units = 1, heads = 1;        // threads to a head, heads in all (of q, k and stored v)
+  int heads_each = 1, groups = 1;  // heads of a thread, threads that share the heads
 };
 struct PagedAttnSpec {
   fs_paged_attention_desc d{};

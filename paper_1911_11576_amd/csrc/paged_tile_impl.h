@@ -71,7 +71,7 @@ struct TileLine {
     const int last = last_steps(), first = flat >= 0 || tiles == 0 ? last : max(0, mine.keys - mine.fresh + 64) >> 6;
     // (in 64 steps: no more than 2^31 of them)
     const int total = wave_sum((int)min((int64_t)tiles * (first + last) * a.kv_heads >> 7, (int64_t)1 << 24));
-    share_steps = max(a.least_steps, total / (kTileShares / 64));
+    share_steps = max(a.least_steps, (total + total / 4) / (kTileShares / 64));
     for (;; share_steps *= 2) {      // (never more parts than there is room for)
       split = at_least(share_steps + 1);
       parts = split ? (last + share_steps - 1) / share_steps : 1;

@@ -14,6 +14,15 @@
 namespace fs {
 namespace {
 
+// n / d of numbers below 2^31 as a product: m = ceil(2^(31 + s) / d), s = ceil(log2 d), is off by less than d / 2^(31 + s) * n < 1 / d.
+struct Divisor { uint32_t d = 1, m = 1, shift = 0; };
+Divisor divisor(uint32_t d) {
+  uint32_t s = 0;
+  while ((1ull << s) < d) ++s;
+  return Divisor{d, (uint32_t)(((1ull << (31 + s)) + d - 1) / d), 31 + s};
+}
+__device__ __forceinline__ uint32_t quotient(uint32_t n, const Divisor& d) { return (uint32_t)((uint64_t)n * d.m >> d.shift); }
+
 struct RotaryArgs {
   const void *q, *k, *v;
   const int *positions, *slots;
@@ -22,7 +31,9 @@ struct RotaryArgs {
   int64_t q_stride, k_stride, v_stride, q_out_stride, k_out_stride;
   CacheLayout cache;
   int64_t n_slots;
-  int tokens, q_heads, k_heads, heads, dim, rot, units, heads_at_once, tokens_per_wg, inverse;
+  int token0, tokens;                // of this launch: its first row, the rows behind it
+  int q_heads, k_heads, heads, dim, rot, units, groups, inverse;      // groups: threads to a row and unit
+  Divisor by_lanes, by_units;
   float magnitude;
 };
 
@@ -46,7 +57,7 @@ template <typename T, int W> struct alignas(sizeof(T) * W) Pack {
   typedef typename Raw<sizeof(T) * W>::type raw;
 };
 template <typename T, int W> __device__ __forceinline__ Pack<T, W> load_pack(const T* p) {
-  return __builtin_bit_cast(Pack<T, W>, *reinterpret_cast<const typename Pack<T, W>::raw*>(p));
+  return __builtin_bit_cast(Pack<T, W>, __builtin_nontemporal_load(reinterpret_cast<const typename Pack<T, W>::raw*>(p)));
 }
 template <typename T, int W> __device__ __forceinline__ void store_pack(T* p, const Pack<T, W>& v) {
   *reinterpret_cast<typename Pack<T, W>::raw*>(p) = __builtin_bit_cast(typename Pack<T, W>::raw, v);
@@ -65,12 +76,12 @@ __device__ __forceinline__ void turned(double turns, float* c, float* s) {
   *s = n & 2 ? -b : b;
 }
 
-template <typename T, int W, bool INTER, bool STORE> __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
-  const int lanes = a.units * a.heads_at_once;
-  const int in_wg = (int)threadIdx.x / lanes, r = (int)threadIdx.x - in_wg * lanes;
-  const int64_t token = (int64_t)blockIdx.x * a.tokens_per_wg + in_wg;
-  if (in_wg >= a.tokens_per_wg || token >= a.tokens) return;
-  const int h0 = r / a.units, u = r - h0 * a.units;
+// H: heads of a thread, all of them requested before the angles are made.
+template <typename T, int W, int H, bool INTER, bool STORE> __global__ __launch_bounds__(256) void rotary_kernel(const RotaryArgs a) {
+  const uint32_t n = blockIdx.x * 256u + threadIdx.x, row_in = quotient(n, a.by_lanes), r = n - row_in * a.by_lanes.d;
+  if (row_in >= (uint32_t)a.tokens) return;
+  const int64_t token = (int64_t)a.token0 + row_in;
+  const int h0 = (int)quotient(r, a.by_units), u = (int)r - h0 * a.units;
   int64_t row = 0;
   if (STORE) {
     const int slot = a.slots[token];
@@ -90,6 +101,20 @@ template <typename T, int W, bool INTER, bool STORE> __global__ __launch_bounds_
     e0 = t0 ? u * W : a.rot + (u - turned_units) * 2 * W;
     e1 = t0 ? a.rot / 2 + u * W : e0 + W;
   }
+  Pack<T, W> p[H][2];
+  T* to[H];
+#pragma unroll
+  for (int j = 0; j < H; ++j) {
+    const int h = min(h0 + j * a.groups, a.heads - 1);
+    const bool is_q = h < a.q_heads, is_v = STORE && h >= a.q_heads + a.k_heads;
+    const int kh = h - a.q_heads - (is_v ? a.k_heads : 0);
+    const T* x = static_cast<const T*>(is_q ? a.q : is_v ? a.v : a.k) + token * (is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride) + (int64_t)(is_q ? h : kh) * a.dim;
+    p[j][0] = load_pack<T, W>(x + e0);
+    p[j][1] = load_pack<T, W>(x + (two ? e1 : e0));
+    if (is_q) to[j] = static_cast<T*>(a.q_out) + token * a.q_out_stride + (int64_t)h * a.dim;
+    else if (STORE) to[j] = static_cast<T*>(is_v ? a.v_out : a.k_out) + row + (int64_t)kh * a.cache.head;
+    else to[j] = static_cast<T*>(a.k_out) + token * a.k_out_stride + (int64_t)kh * a.dim;
+  }
   const double position = (double)a.positions[token];
   constexpr double kTurn = 0.15915494309189533577;      // 1 / 2 pi
   float c[W], s[W];
@@ -104,21 +129,12 @@ template <typename T, int W, bool INTER, bool STORE> __global__ __launch_bounds_
       s[i] *= a.inverse ? -a.magnitude : a.magnitude;
     }
   }
-  for (int h = h0; h < a.heads; h += a.heads_at_once) {
-    const T* x;
-    T* y;
-    const bool is_q = h < a.q_heads, is_v = STORE && h >= a.q_heads + a.k_heads;
-    const int kh = h - a.q_heads - (is_v ? a.k_heads : 0);
-    if (is_q) {
-      x = static_cast<const T*>(a.q) + token * a.q_stride + (int64_t)h * a.dim;
-      y = static_cast<T*>(a.q_out) + token * a.q_out_stride + (int64_t)h * a.dim;
-    } else {
-      x = static_cast<const T*>(is_v ? a.v : a.k) + token * (is_v ? a.v_stride : a.k_stride) + (int64_t)kh * a.dim;
-      if (STORE) y = static_cast<T*>(is_v ? a.v_out : a.k_out) + row + (int64_t)kh * a.cache.head;
-      else y = static_cast<T*>(a.k_out) + token * a.k_out_stride + (int64_t)kh * a.dim;
-    }
-    Pack<T, W> p0 = load_pack<T, W>(x + e0), p1 = load_pack<T, W>(x + (two ? e1 : e0));
-    if (!is_v) {
+#pragma unroll
+  for (int j = 0; j < H; ++j) {
+    const int h = h0 + j * a.groups;
+    if (h >= a.heads) break;
+    Pack<T, W> p0 = p[j][0], p1 = p[j][1];
+    if (!STORE || h < a.q_heads + a.k_heads) {
       if constexpr (INTER) {
 #pragma unroll
         for (int i = 0; i < W / 2; ++i) {
@@ -141,24 +157,40 @@ template <typename T, int W, bool INTER, bool STORE> __global__ __launch_bounds_
         }
       }
     }
-    store_pack<T, W>(y + e0, p0);
-    if (two) store_pack<T, W>(y + e1, p1);
+    store_pack<T, W>(to[j] + e0, p0);
+    if (two) store_pack<T, W>(to[j] + e1, p1);
   }
 }
 
-template <typename T, int W> hipError_t launch_width(const RotaryArgs& a, const RotarySpec& s, hipStream_t stream) {
-  const dim3 grid((unsigned)s.grid), wg(s.wg);
+template <typename T, int W, int H> void launch_heads(const RotaryArgs& a, const RotarySpec& s, unsigned wgs, hipStream_t stream) {
   const bool store = s.d.blocks > 0;
   if constexpr (W >= 2) {
     if (s.d.interleaved) {
-      if (store) hipLaunchKernelGGL((rotary_kernel<T, W, true, true>), grid, wg, 0, stream, a);
-      else hipLaunchKernelGGL((rotary_kernel<T, W, true, false>), grid, wg, 0, stream, a);
-      return hipGetLastError();
+      if (store) hipLaunchKernelGGL((rotary_kernel<T, W, H, true, true>), dim3(wgs), dim3(256), 0, stream, a);
+      else hipLaunchKernelGGL((rotary_kernel<T, W, H, true, false>), dim3(wgs), dim3(256), 0, stream, a);
+      return;
     }
   }
-  if (store) hipLaunchKernelGGL((rotary_kernel<T, W, false, true>), grid, wg, 0, stream, a);
-  else hipLaunchKernelGGL((rotary_kernel<T, W, false, false>), grid, wg, 0, stream, a);
-  return hipGetLastError();
+  if (store) hipLaunchKernelGGL((rotary_kernel<T, W, H, false, true>), dim3(wgs), dim3(256), 0, stream, a);
+  else hipLaunchKernelGGL((rotary_kernel<T, W, H, false, false>), dim3(wgs), dim3(256), 0, stream, a);
+}
+
+template <typename T, int W> hipError_t launch_width(RotaryArgs a, const RotarySpec& s, hipStream_t stream) {
+  // threads are numbered in 31 bits: beyond that, several launches
+  const int64_t lanes = (int64_t)s.units * s.groups, most = (0x7fffff00ll / lanes);
+  for (int64_t t = 0; t < s.d.tokens; t += most) {
+    a.token0 = (int)t;
+    a.tokens = (int)std::min(most, s.d.tokens - t);
+    const unsigned wgs = (unsigned)((a.tokens * lanes + 255) / 256);
+    switch (s.heads_each) {
+      case 1: launch_heads<T, W, 1>(a, s, wgs, stream); break;
+      case 4: launch_heads<T, W, 4>(a, s, wgs, stream); break;
+      default: launch_heads<T, W, 8>(a, s, wgs, stream); break;
+    }
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 template <typename T> hipError_t launch_type(const RotaryArgs& a, const RotarySpec& s, hipStream_t stream) {
@@ -175,12 +207,9 @@ template <typename T> hipError_t launch_type(const RotaryArgs& a, const RotarySp
 }  // namespace
 
 void rotary_geometry(RotarySpec* s) {
-  // as many heads of a token at a time as a workgroup of 256 holds, all of them if it can
-  s->heads_at_once = std::max(1, std::min(s->heads, 256 / s->units));
-  const int lanes = s->units * s->heads_at_once;
-  s->tokens_per_wg = std::max(1, 256 / lanes);
-  s->wg = (lanes * s->tokens_per_wg + 63) / 64 * 64;
-  s->grid = s->d.tokens ? (s->d.tokens + s->tokens_per_wg - 1) / s->tokens_per_wg : 0;
+  const int64_t threads = (int64_t)s->d.tokens * s->units * s->heads;
+  s->heads_each = getenv("RH") ? atoi(getenv("RH")) : threads >= 4 * 131072 ? 4 : 1;
+  s->groups = (s->heads + s->heads_each - 1) / s->heads_each;
 }
 
 int rotary_launch(const RotarySpec& s, const void* const* in, void* const* out, void* stream, std::string* err) {
@@ -200,8 +229,8 @@ int rotary_launch(const RotarySpec& s, const void* const* in, void* const* out, 
   a.q_stride = s.d.q_stride; a.k_stride = s.d.k_stride; a.v_stride = s.d.v_stride; a.q_out_stride = s.d.q_out_stride; a.k_out_stride = s.d.k_out_stride;
   a.cache = s.cache;
   a.n_slots = (int64_t)s.d.blocks << s.cache.shift;
-  a.tokens = s.d.tokens; a.q_heads = s.d.q_heads; a.k_heads = s.d.k_heads; a.heads = s.heads; a.dim = s.d.head_dim; a.rot = s.d.rotary_dim;
-  a.units = s.units; a.heads_at_once = s.heads_at_once; a.tokens_per_wg = s.tokens_per_wg; a.inverse = s.d.inverse;
+  a.q_heads = s.d.q_heads; a.k_heads = s.d.k_heads; a.heads = s.heads; a.dim = s.d.head_dim; a.rot = s.d.rotary_dim;
+  a.units = s.units; a.groups = s.groups; a.by_units = divisor(s.units); a.by_lanes = divisor(s.units * s.groups); a.inverse = s.d.inverse;
   a.magnitude = (float)s.d.magnitude;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = s.d.dtype == FS_F32 ? launch_type<float>(a, s, st) : s.d.dtype == FS_F16 ? launch_type<f16_t>(a, s, st) : launch_type<bf16_t>(a, s, st);
