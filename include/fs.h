@@ -485,12 +485,12 @@ fs_status fs_rotary_frequencies(int32_t rotary_dim, double base, double factor, 
  *             0 the caller gives fs_launch a device buffer of that size as ONE MORE OUTPUT, behind the others; nothing
  *             in it has to start at zero, and launches with buffers of their own may overlap in time.
  * Rows outside every request are left as they were.  A length beyond the table's row counts as that row's, one below 0 as 0;
- * starts are cut to [0, tokens] and a run that ends before it begins is empty.  Keys in blocks outside [0, blocks) are not
+ * starts are cut to [0, tokens], a run that ends before it begins is empty, and rows that several requests claim are undefined.  Keys in blocks outside [0, blocks) are not
  * seen.  What lies in the cache behind a request's length is never used, whatever it is, and an infinity or NaN in a value
  * reaches only the rows that see it.
  * max_new: the most new tokens that a request has, for the choice of kernels (0: unknown); a request may have more.
  * FS_F16 or FS_BF16 (the probabilities are rounded to it for the second product, all sums are fp32), head_dim 32, 64, 96 or
- * 128, strides and head strides multiples of 8.  Results do not depend on timing: no atomics, a fixed order of sums.
+ * 128, strides and head strides multiples of 8, up to 65536 requests, 2^30 keys in a row of the table.  Results do not depend on timing: no atomics, a fixed order of sums.
  * Errors: FS_ERR_INVALID, FS_ERR_UNSUPPORTED (a head_dim or stride that no kernel takes), FS_ERR_NOMEM. */
 typedef struct {
   int32_t dtype;                   /* FS_F16 or FS_BF16: q, caches, out */

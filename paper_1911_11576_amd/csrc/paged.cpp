@@ -218,7 +218,7 @@ fs_status fs_plan_create_paged_attention(const fs_paged_attention_desc* desc, in
     fs_paged_attention_desc& d = s.d;
     if (d.reserved) { *err = "reserved must be 0"; return false; }
     if (d.dtype != FS_F32 && d.dtype != FS_F16 && d.dtype != FS_BF16) { *err = "unknown dtype"; return false; }
-    if (d.requests < 0 || d.requests > (1 << 20)) { *err = "requests out of range [0,2^20]"; return false; }
+    if (d.requests < 0 || d.requests > 65536) { *err = "requests out of range [0,65536]"; return false; }
     if (d.q_heads < 1 || d.kv_heads < 1 || d.q_heads % d.kv_heads || d.q_heads > 65536) { *err = "q_heads must be a multiple of kv_heads, both above 0 and up to 65536"; return false; }
     if (d.tokens < 0 || (int64_t)d.tokens * d.q_heads > kMostTokens) { *err = "tokens below 0, or tokens * q_heads beyond 2^30"; return false; }
     if (d.head_dim < 1) { *err = "head_dim must be above 0"; return false; }
@@ -227,7 +227,7 @@ fs_status fs_plan_create_paged_attention(const fs_paged_attention_desc* desc, in
     if ((d.causal | 1) != 1 || (d.log_sum_exp | 1) != 1) { *err = "causal and log_sum_exp are 0 or 1"; return false; }
     if (d.window < 0 || (d.window && !d.causal)) { *err = "window below 0, or without causal"; return false; }
     if (d.max_new < 0) { *err = "max_new below 0"; return false; }
-    if (!std::isfinite(d.scale) || !std::isfinite((float)d.scale)) { *err = "scale must be finite in fp32"; return false; }
+    if (!std::isfinite((float)(d.scale * 1.4426950408889634))) { *err = "scale must be finite in fp32"; return false; }
     const int64_t t = d.tokens, dim = d.head_dim, row = d.q_heads * dim;
     if (!token_stride(&d.q_stride, d.q_heads, dim, "q_stride", err) || !token_stride(&d.out_stride, d.q_heads, dim, "out_stride", err)) return false;
     int64_t cache_bytes = 0;

@@ -64,7 +64,7 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.q_stride = s.d.q_stride; a.out_stride = s.d.out_stride;
   a.cache = s.cache;
   if (s.partial_bytes) a.partial = static_cast<float*>(out[s.d.log_sum_exp ? 2 : 1]);
-  a.requests = s.d.requests; a.tokens = s.d.tokens; a.q_heads = s.d.q_heads; a.kv_heads = s.d.kv_heads; a.share = s.share; a.causal = s.d.causal; a.window = s.d.window;
+  a.requests = s.d.requests; a.tokens = s.d.tokens; a.q_heads = s.d.q_heads; a.kv_heads = s.d.kv_heads; a.share = s.share; a.causal = s.d.causal; a.window = std::min(s.d.window, 1 << 30);      // (no request has more keys)
   a.width = s.d.blocks ? s.d.table_blocks : 0;      // (without a block there is no key to see, and no address to read)
   a.scale2 = (float)(s.d.scale * 1.4426950408889634);
   if (a.scale2 == 0.f) a.scale2 = 1.17549435e-38f;      // (what is not seen is -inf times the scale)

@@ -57,14 +57,14 @@ template <int NT> struct FewLine {
   __device__ __forceinline__ int groups() const {
     return min(a.log_groups, 31 - __clz((int)max(total, 1u)));
   }
-  struct Tile { int b, head, row0, unit, n_units; uint32_t first; PagedRequest r; };      // first: the tile's first unit in the line
+  struct Tile { int b, head, row0, unit, n_units; uint32_t first; PagedRequest r; bool there; };      // first: the tile's first unit in the line
   __device__ __forceinline__ Tile find(uint32_t unit) {
     while (unit >= before + all && base + 64 < a.requests) {
       before += all;
       load(base + 64);
     }
     const uint64_t behind = __ballot(before + upto <= unit);
-    const int lane = __popcll(behind);
+    const int lane = min(63, (int)__popcll(behind));
     Tile t;
     t.b = base + lane;
     t.r = PagedRequest{__builtin_amdgcn_readlane(mine.first, lane), __builtin_amdgcn_readlane(mine.fresh, lane), __builtin_amdgcn_readlane(mine.keys, lane)};
@@ -73,8 +73,10 @@ template <int NT> struct FewLine {
     const uint32_t tile = (unit - start) / (uint32_t)t.n_units, tiles = (uint32_t)(t.r.fresh * a.share + 16 * NT - 1) / (16 * NT);
     t.unit = (int)(unit - start - tile * t.n_units);
     t.first = unit - t.unit;
-    t.head = (int)(tile / tiles);
+    t.head = tiles ? (int)(tile / tiles) : 0;
     t.row0 = (int)(tile - t.head * tiles) * 16 * NT;
+    // (requests whose rows overlap can be more units than 32 bits number: then what was found may be no tile)
+    t.there = t.b < a.requests && (unsigned)t.head < (unsigned)a.kv_heads && t.row0 >= 0 && t.row0 < t.r.fresh * a.share;
     return t;
   }
 };
@@ -123,6 +125,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
 
   for (uint32_t cur = u0; cur < u1;) {
     const auto tile = line.find(cur);
+    if (!tile.there) break;
     const int n = min(tile.n_units - tile.unit, (int)(u1 - cur));
     const PagedRequest r = tile.r;
     const int rows = r.fresh * a.share;
@@ -396,9 +399,9 @@ template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_j
   if (at >= line.total) return;
   const auto tile = line.find(at);
   const uint32_t first = tile.first, end = first + tile.n_units, before = line.cut(p - 1, log_groups);
-  if (at == first || before > first) return;      // no part before the cut, or another cut is the first
+  if (!tile.there || at == first || before > first) return;      // no part before the cut, or another cut is the first
   int last = p;                                   // the workgroup that the last part is of
-  while (line.cut(last + 1, log_groups) < end) ++last;
+  while (last + 1 < 1 << log_groups && line.cut(last + 1, log_groups) < end) ++last;
   const int e = run * 256 + lane * 4, row = e / D;
   const int n = last - p + 2;
   auto part = [&](int k) { return a.partial + (2 * (p - 1 + k) + (k == 0 && before != first ? 1 : 0)) * kFloats; };

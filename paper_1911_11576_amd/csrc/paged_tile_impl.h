@@ -188,6 +188,7 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile(const Pa
       else if (!line.find_whole(k - line.items, &work)) return;
     }
   }
+  if (work.row0 < 0 || work.row0 >= work.rows) return;      // (requests whose rows overlap can be more tiles than 32 bits number)
   const PagedRequest r = work.r;
   const int head = work.head;
   // a part's steps: an even run of the tile's
@@ -429,7 +430,7 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile_join(con
     const float* at = a.tile_partial + (int64_t)work.partial * (128 * (D + 2));
     for (int i = threadIdx.x; i < 1024; i += blockDim.x) {
       const int e = (run * 1024 + i) * 4, mine = e / D, row = work.row0 + mine;
-      if (row >= work.rows) continue;
+      if (row < 0 || row >= work.rows) continue;
       FewSum s{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
       auto part = [&](int n) { return at + n * stride; };
       int n = 0;

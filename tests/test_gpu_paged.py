@@ -362,6 +362,41 @@ def test_attention_odd_lengths(lengths, starts):
     check_attention(c)
 
 
+@pytest.mark.parametrize("starts", [[0, 9, 0, 9], [9, 0, 9, 0], [5, 5, 1, 9], [0, 9, 9, 9]])
+@pytest.mark.parametrize("max_new", [0, 1])
+def test_attention_rows_of_several_requests(starts, max_new):
+    """Rows that no request or only one has are right whatever the others claim."""
+    c = problem(np.random.default_rng(14), "bf16", [40, 40, 40], [3, 3, 3], 48, 3, 64, 16)
+    c["starts"] = np.array(starts)
+    claims = np.array([sum(starts[b] <= t < starts[b + 1] for b in range(3)) for t in range(9)])
+    plan, nbytes = plan_of(c, max_new=max_new)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+    want = [a[claims < 2] for a in wanted(c)]
+    check_out(dict(c, q=c["q"][claims < 2]), [outs[0][claims < 2], outs[1][claims < 2]], want, f"starts {starts}")
+
+
+@pytest.mark.parametrize("q_heads, kv_heads", [(64, 1), (33, 1), (24, 1), (7, 7)])
+@pytest.mark.parametrize("requests", [3, 70, 130])
+def test_attention_of_many_requests(q_heads, kv_heads, requests):
+    """More requests than a wavefront has lanes, single tokens and chunks among each other, runs of heads beyond a tile's rows."""
+    rng = np.random.default_rng(requests)
+    new = [int(n) for n in rng.choice([0, 1, 1, 2, 5, 40], requests)]
+    keys = [n + int(k) for n, k in zip(new, rng.choice([0, 1, 30, 200], requests))]
+    c = problem(rng, "bf16", keys, new, q_heads, kv_heads, 32, 16, order="token", pad_rows=2)
+    check_attention(c)
+    check_attention(c, window=2**31 - 1)
+
+
+@pytest.mark.parametrize("new", [1, 2, 60])
+def test_attention_of_one_long_request(new):
+    """Keys of one tile over many workgroups: the parts are joined in the order of the keys."""
+    c = problem(np.random.default_rng(15), "bf16", [40000, 3], [new, 1], 4, 1, 128, 64)
+    check_attention(c, max_new=new)
+    check_attention(c, max_new=new, window=20000)
+
+
 @pytest.mark.parametrize("new, keys", [(3, 40), (70, 200), (150, 150)])
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
 def test_attention_values_that_some_rows_do_not_see(new, keys, value):
@@ -518,6 +553,25 @@ def test_steps_of_a_server():
             within(out[starts[b]:starts[b + 1]], want, (u + 2 * off[..., None]) * weight + u * np.abs(want), f"step {step} request {b}")
         s.next()
     assert len(given[4]) > 90      # its prompt is through, single tokens followed
+
+
+def test_two_launches_of_a_plan_at_once():
+    """On two streams, with outputs and partial results of their own."""
+    c = problem(np.random.default_rng(16), "f16", [5000, 700, 20000], [1, 1, 30], 8, 2, 64, 16)
+    plan, nbytes = plan_of(c, max_new=0)
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    with plan:
+        ins, sets = inputs(c), [buffers(c, nbytes) for _ in range(2)]
+        alone = buffers(c, nbytes)
+        plan.launch(ins, alone)
+        torch.cuda.synchronize()
+        for _ in range(5):
+            for s, outs in zip(streams, sets):
+                plan.launch(ins, outs, s.cuda_stream)
+        torch.cuda.synchronize()
+    for outs in sets:
+        assert torch.equal(outs[0], alone[0]) and torch.equal(outs[1], alone[1])
+    check_out(c, alone, wanted(c), "two streams")
 
 
 def test_steps_in_a_graph():

@@ -45,7 +45,7 @@ def test_rotary_refused(change, text):
 @pytest.mark.parametrize("change, text", [
     (dict(requests=-1), "requests"), (dict(tokens=-1), "tokens"), (dict(tokens=2**30), "tokens"), (dict(q_heads=3), "q_heads"), (dict(kv_heads=0), "kv_heads"),
     (dict(head_dim=0), "head_dim"), (dict(block_size=12), "power of two"), (dict(blocks=2**28), "2^31"), (dict(table_blocks=2**28), "2^31"), (dict(causal=2), "0 or 1"),
-    (dict(window=-1), "window"), (dict(window=5, causal=False), "window"), (dict(max_new=-1), "max_new"), (dict(scale=float("inf")), "scale"),
+    (dict(window=-1), "window"), (dict(window=5, causal=False), "window"), (dict(max_new=-1), "max_new"), (dict(scale=float("inf")), "scale"), (dict(scale=3e38), "scale"), (dict(requests=65537), "requests"),
     (dict(q_stride=128), "q_stride"), (dict(out_stride=-8), "out_stride"), (dict(slot_stride=32, head_stride=1024, block_stride=4096), "overlap")])
 def test_attention_refused(change, text):
     refused(Plan.paged_attention, binding.FS_ERR_INVALID, text, **dict(ATTENTION, **change))
