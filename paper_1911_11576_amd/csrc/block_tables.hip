@@ -20,68 +20,93 @@ struct TablesArgs {
   int requests, tokens, blocks, shift, width, n_free;
 };
 
-// Sum over the threads before this one; `room` has a place per wavefront, and *all gets the workgroup's total.
-template <int WG> __device__ __forceinline__ uint64_t block_exclusive(uint64_t v, uint64_t* room, uint64_t* all) {
+// Sums stop at 2^32 - 1: everything beyond `tokens` is cut to it anyway.
+__device__ __forceinline__ uint32_t add(uint32_t a, uint32_t b) { return __builtin_elementwise_add_sat(a, b); }
+template <int CTRL, int ROWS> __device__ __forceinline__ uint32_t moved(uint32_t v) { return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xF, false); }
+
+// Sum over the threads before this one, by shifts inside rows of 16 lanes, then the last lane of the row before and of the half before;
+// `room` has a place per wavefront, and *all gets the workgroup's total.
+template <int WG> __device__ __forceinline__ uint32_t block_exclusive(uint32_t v, uint32_t* room, uint32_t* all) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  uint64_t s = v;
-#pragma unroll
-  for (int d = 1; d < 64; d <<= 1) {
-    const uint64_t t = __shfl_up((unsigned long long)s, d);
-    if (lane >= d) s += t;
-  }
+  uint32_t s = v;
+  s = add(s, moved<0x111, 0xF>(s));
+  s = add(s, moved<0x112, 0xF>(s));
+  s = add(s, moved<0x114, 0xF>(s));
+  s = add(s, moved<0x118, 0xF>(s));
+  s = add(s, moved<0x142, 0xA>(s));
+  s = add(s, moved<0x143, 0xC>(s));
+  uint32_t before = __shfl_up(s, 1);
+  if (lane == 0) before = 0;
   if constexpr (WG == 64) {
-    *all = __shfl((unsigned long long)s, 63);
-    return s - v;
+    *all = __builtin_amdgcn_readlane(s, 63);
+    return before;
   }
   if (lane == 63) room[w] = s;
   __syncthreads();
-  uint64_t before = s - v, total = 0;
+  uint32_t total = 0;
 #pragma unroll
   for (int k = 0; k < WG / 64; ++k) {
-    if (k < w) before += room[k];
-    total += room[k];
+    const uint32_t n = room[k];
+    if (k < w) before = add(before, n);
+    total = add(total, n);
   }
   *all = total;
   __syncthreads();
   return before;
 }
 
-template <int WG> __global__ __launch_bounds__(WG) void block_tables_kernel(const TablesArgs a) {
-  extern __shared__ uint64_t smem[];
-  uint64_t* room = smem;                            // [4]
-  uint32_t* starts = reinterpret_cast<uint32_t*>(smem + 4);      // [requests + 1]
+// E: requests of a thread, whose lengths it keeps.
+template <int WG, int E> __global__ __launch_bounds__(WG) void block_tables_kernel(const TablesArgs a) {
+  extern __shared__ uint32_t smem[];
+  uint32_t* room = smem;                            // [16]
+  uint32_t* starts = smem + 16;                     // [requests + 1]
   uint32_t* first_free = starts + a.requests + 1;   // [requests], place of a request's first new block in the free list
+  uint32_t* in_cache = first_free + a.requests;     // [requests], its cached tokens
   const uint32_t T = (uint32_t)a.tokens;
   const int most = (int)min((int64_t)a.width << a.shift, (int64_t)0x7fffffff);
   const uint32_t in_block = (1u << a.shift) - 1;
-  const int each = (a.requests + WG - 1) / WG;
-  const int r0 = min((int)threadIdx.x * each, a.requests), r1 = min(r0 + each, a.requests);
-  auto cached_of = [&](int r) { return max(0, min(a.cached[r], most)); };
-  auto fresh_of = [&](int r, int c) { return (uint32_t)min(max(a.fresh[r], 0), most - c); };
-  uint64_t mine = 0, all;
-  for (int r = r0; r < r1; ++r) mine += fresh_of(r, cached_of(r));
-  uint32_t at = (uint32_t)min(block_exclusive<WG>(mine, room, &all), (uint64_t)T), blocks = 0;
+  const int r0 = (int)threadIdx.x * E;
+  uint32_t c[E], f[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int r = min(r0 + i, a.requests - 1);
+    c[i] = a.requests ? (uint32_t)max(0, min(a.cached[r], most)) : 0;
+    f[i] = a.requests ? (uint32_t)max(a.fresh[r], 0) : 0;
+  }
+  uint32_t mine = 0, all;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    f[i] = r0 + i < a.requests ? min(f[i], (uint32_t)most - c[i]) : 0;
+    mine = add(mine, f[i]);
+  }
+  uint32_t at = min(block_exclusive<WG>(mine, room, &all), T), blocks = 0, first[E];
   // the requests' rows, and the blocks they need new
-  for (int r = r0; r < r1; ++r) {
-    const int c = cached_of(r);
-    const uint32_t next = (uint32_t)min((uint64_t)T, (uint64_t)at + fresh_of(r, c));
-    starts[r] = at;
-    first_free[r] = blocks;
-    blocks += (((uint32_t)c + (next - at) + in_block) >> a.shift) - (((uint32_t)c + in_block) >> a.shift);
-    if (blockIdx.x == 0) {
-      a.starts[r] = (int)at;
-      a.lengths[r] = c + (int)(next - at);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const int r = r0 + i;
+    const uint32_t next = min(T, add(at, f[i]));
+    first[i] = blocks;
+    blocks += ((c[i] + (next - at) + in_block) >> a.shift) - ((c[i] + in_block) >> a.shift);
+    if (r < a.requests) {
+      starts[r] = at;
+      in_cache[r] = c[i];
+      if (blockIdx.x == 0) {
+        a.starts[r] = (int)at;
+        a.lengths[r] = (int)(c[i] + (next - at));
+      }
     }
     at = next;
   }
-  if (threadIdx.x == WG - 1) starts[a.requests] = at;      // (the last thread's run ends where the requests do, or is empty behind them)
-  const uint32_t blocks_before = (uint32_t)block_exclusive<WG>(blocks, room, &all);
-  for (int r = r0; r < r1; ++r) first_free[r] += blocks_before;
+  if (threadIdx.x == WG - 1) starts[a.requests] = at;      // (behind the last request nothing is added)
+  const uint32_t blocks_before = block_exclusive<WG>(blocks, room, &all);
+#pragma unroll
+  for (int i = 0; i < E; ++i)
+    if (r0 + i < a.requests) first_free[r0 + i] = blocks_before + first[i];
   __syncthreads();
   const uint32_t total = starts[a.requests];
   if (blockIdx.x == 0 && threadIdx.x == 0) {
     a.starts[a.requests] = (int)total;
-    a.taken[0] = (int)min(all, (uint64_t)a.n_free);
+    a.taken[0] = (int)min(all, (uint32_t)a.n_free);
     a.taken[1] = (int)all;
   }
   for (uint32_t t = blockIdx.x * WG + threadIdx.x; t < T; t += gridDim.x * WG) {
@@ -92,7 +117,7 @@ template <int WG> __global__ __launch_bounds__(WG) void block_tables_kernel(cons
         const int mid = (lo + hi) >> 1;
         if (starts[mid] <= t) lo = mid; else hi = mid;
       }
-      const uint32_t c = (uint32_t)cached_of(lo), p = c + (t - starts[lo]), entry = p >> a.shift, have = (c + in_block) >> a.shift;
+      const uint32_t c = in_cache[lo], p = c + (t - starts[lo]), entry = p >> a.shift, have = (c + in_block) >> a.shift;
       int* row = a.tables + (int64_t)lo * a.width;
       int block;
       if (entry < have) {
@@ -116,8 +141,11 @@ int block_tables_launch(const BlockTablesSpec& s, const void* const* in, void* c
   const auto i = [&](int k) { return static_cast<const int*>(in[k]); };
   const auto o = [&](int k) { return static_cast<int*>(out[k]); };
   const TablesArgs a{i(0), i(1), i(2), o(0), o(1), o(2), o(3), o(4), o(5), s.d.requests, s.d.tokens, s.d.blocks, __builtin_ctz((unsigned)s.d.block_size), s.d.table_blocks, s.d.free_blocks};
-  if (s.wg == 64) hipLaunchKernelGGL(block_tables_kernel<64>, dim3(s.grid), dim3(64), (size_t)s.lds, static_cast<hipStream_t>(stream), a);
-  else hipLaunchKernelGGL(block_tables_kernel<256>, dim3(s.grid), dim3(256), (size_t)s.lds, static_cast<hipStream_t>(stream), a);
+  const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(s.grid), dim3(s.wg), (size_t)s.lds, static_cast<hipStream_t>(stream), a); };
+  if (s.wg == 64) launch(block_tables_kernel<64, 1>);
+  else if (s.wg == 256) launch(block_tables_kernel<256, 1>);
+  else if (s.d.requests <= 1024) launch(block_tables_kernel<1024, 1>);
+  else launch(block_tables_kernel<1024, 4>);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) { *err = std::string("block_tables launch: ") + hipGetErrorString(e); return -1; }
   return 0;

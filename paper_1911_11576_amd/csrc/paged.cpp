@@ -104,12 +104,11 @@ fs_status fs_plan_create_block_tables(const fs_block_tables_desc* desc, fs_plan*
     if (!blocks_fit(d.blocks, d.block_size, &shift, err) || !blocks_fit(d.table_blocks, d.block_size, &shift, err)) return false;
     fs::BlockTablesSpec& s = p->paged.tables;
     s.d = d;
-    // Every workgroup scans all requests for itself (the two scans are a few hundred clocks a thousand requests) and serves a
-    // run of rows: one for a decode step, enough of them for a chunk's rows.
-    s.wg = d.requests <= 64 && d.tokens <= 64 ? 64 : 256;
-    const int64_t rows = 512;
-    s.grid = (int)std::min<int64_t>(std::max<int64_t>(1, (d.tokens + rows - 1) / rows), 1024);
-    s.lds = 8ll * (d.requests + 1) + 256;
+    // Every workgroup scans all requests for itself and serves a row a thread.  One wavefront for a decode step; else a thread a
+    // request where a workgroup has so many (515 requests, 32768 rows: 5.7 us with three requests and two rows to one of 256 threads).
+    s.wg = d.requests <= 64 && d.tokens <= 64 ? 64 : d.requests <= 256 ? 256 : 1024;
+    s.grid = (int)std::min<int64_t>(std::max<int64_t>(1, ((int64_t)d.tokens + s.wg - 1) / s.wg), 2048);
+    s.lds = 12ll * (d.requests + 1) + 64;
     p->lds_bytes = s.lds;
     const int64_t b = d.requests, t = d.tokens;
     p->paged.kind = FS_SCHED_BLOCK_TABLES;

@@ -447,8 +447,9 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile_join(con
 }
 
 // Requests of few rows and of many in one launch, and one that joins the parts of both: the former read memory while the latter keep the
-// matrix unit busy, and where there are none of them (whole prompts) they cost no launches of their own.
-template <typename T, int D, int NT> __global__ __launch_bounds__(256, 2) void paged_mixed_kernel(const PagedArgs a) {
+// matrix unit busy, and where there are none of them (whole prompts) they cost no launches of their own.  Four workgroups to a CU up to head dim
+// 64 (prompts of 2048 rows x 16 heads of 64: 60.5 us, 66.6 with three); beyond, two is what the LDS holds.
+template <typename T, int D, int NT> __global__ __launch_bounds__(256, (D <= 64 && NT == 1 ? 4 : 2)) void paged_mixed_kernel(const PagedArgs a) {
   __shared__ __align__(1024) union { FewLds<D, NT, 4> few; TileShared<D> tile; } lds;
   const int tiles = gridDim.x - a.few_grid, b = blockIdx.x;
   if (b < tiles) paged_tile<T, D>(a, lds.tile, b);
