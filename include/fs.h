@@ -485,7 +485,7 @@ fs_status fs_rotary_frequencies(int32_t rotary_dim, double base, double factor, 
  *             0 the caller gives fs_launch a device buffer of that size as ONE MORE OUTPUT, behind the others; nothing
  *             in it has to start at zero, and launches with buffers of their own may overlap in time.
  * Rows outside every request are left as they were.  A length beyond the table's row counts as that row's, one below 0 as 0;
- * starts are cut to [0, tokens], a run that ends before it begins is empty, and rows that several requests claim are undefined.  Keys in blocks outside [0, blocks) are not
+ * starts are cut to [0, tokens]; they do not decrease (where they do, the rows concerned are undefined).  Keys in blocks outside [0, blocks) are not
  * seen.  What lies in the cache behind a request's length is never used, whatever it is, and an infinity or NaN in a value
  * reaches only the rows that see it.
  * max_new: the most new tokens that a request has, for the choice of kernels (0: unknown); a request may have more.

@@ -15,13 +15,15 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   s->row_tiles = (many ? s->share : rows) <= 16 ? 1 : 2;
   s->few_rows = many ? 16 * s->row_tiles : 1 << 30;
   const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;      // at most
-  const int64_t m = 16 * s->row_tiles, waves = many ? 4 : 8;
+  const int64_t m = 16 * s->row_tiles;
+  int64_t waves = many ? 4 : 8;      // of a workgroup
   const bool any = d.tokens && d.requests;
   if (!many && keys <= 1024 && tiles <= 65536) {
     // no request is longer than four steps: a workgroup each tile, nothing to join
     s->log_groups = -1;
     s->unit_keys = 1024;
     s->few_grid = (int)tiles;
+    if (tiles > 256) waves = 4;
   } else {
     // as many wavefronts as the chip holds, eight to a CU
     s->log_groups = many ? 9 : 8;
@@ -48,7 +50,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
 
 std::string paged_attn_describe(const PagedAttnSpec& s) {
   char buf[320];
-  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=%d%s", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.slots ? 256 : 512,
+  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=%d%s", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.slots || (s.log_groups < 0 && s.few_grid > 256) ? 256 : 512,
                    s.log_groups < 0 ? "" : "; join[GRID,CTA]");
   if (s.slots) snprintf(buf + n, sizeof buf - n, "; requests of more than %d rows: rows to a tile=128, cta_num=%lld", s.few_rows, (long long)(s.slots * s.d.kv_heads));
   return buf;

@@ -46,6 +46,24 @@ __device__ __forceinline__ int paged_first_key(const PagedArgs& a, const PagedRe
   return a.window ? max(0, r.keys - r.fresh + 1 - a.window) & ~31 : 0;
 }
 
+// The request to which place `at` of a line of tiles of 1 << log_rows rows belongs in which request b's begin at place
+// first * share / rows + b: as many places as it can have tiles, whatever the lengths of the others.  -1: none.
+__device__ __forceinline__ int paged_place(const PagedArgs& a, int b, int log_rows) {
+  return (int)((int64_t)min(max(a.starts[b], 0), a.tokens) * a.share >> log_rows) + b;
+}
+__device__ __forceinline__ int paged_find(const PagedArgs& a, int at, int log_rows) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = a.requests;      // among n requests from lo on, 64 of them looked at at a time
+  for (;;) {
+    const int step = (n + 63) >> 6, b = lo + lane * step;
+    const int here = __popcll(__ballot(b < lo + n && paged_place(a, min(b, a.requests - 1), log_rows) <= at));
+    if (here == 0) return -1;
+    lo += (here - 1) * step;
+    if (step == 1) return lo;
+    n = min(step, a.requests - lo);
+  }
+}
+
 // Sum over the wavefront's lanes, the same in all of them.
 __device__ __forceinline__ int wave_sum(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);

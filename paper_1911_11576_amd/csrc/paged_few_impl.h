@@ -13,17 +13,16 @@
 namespace fs {
 
 
-constexpr int kFewWaves = 8;      // of a workgroup, which is a CU's
-
 // Partial results of a workgroup: its first run of a tile and its last, each M rows of D sums, M maxima, M sums of exponentials.
 template <int D, int NT> struct FewPart { static constexpr int kRows = 16 * NT, kFloats = kRows * (D + 2); };
 
-// The line of units.  Every wavefront walks it for itself, 64 requests at a time, one a lane.
+// The line of units.  Every wavefront looks at it for itself, 64 requests at a time, one a lane.
 template <int NT> struct FewLine {
   const PagedArgs& a;
   uint32_t total = 0;
+  uint32_t chunks_upto = 0;      // units up to and with the lane's 64 requests, of the first 4096
   // the 64 requests from `base` on: units before the first, and a lane's: those up to and with its own
-  int base = 0;
+  int base = -1;
   uint32_t before = 0, upto = 0, all = 0;
   PagedRequest mine{};
   uint32_t units = 0;
@@ -32,36 +31,79 @@ template <int NT> struct FewLine {
   __device__ __forceinline__ int key_units(const PagedRequest& r) const {
     return max(1, (r.keys - paged_first_key(a, r) + a.unit_keys - 1) / a.unit_keys);
   }
+  __device__ __forceinline__ uint32_t units_of(const PagedRequest& r) const {
+    if (r.fresh * a.share > a.few_rows) return 0;
+    return (uint32_t)((r.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(r) * (uint32_t)a.kv_heads;
+  }
+  __device__ __forceinline__ PagedRequest request(int b) const { return b < a.requests ? paged_request(a, b) : PagedRequest{}; }
   __device__ __forceinline__ void load(int from) {
-    const int b = from + (int)(threadIdx.x & 63);
     base = from;
-    units = 0;
-    if (b < a.requests) {
-      mine = paged_request(a, b);
-      if (mine.fresh * a.share <= a.few_rows) units = (uint32_t)((mine.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(mine) * (uint32_t)a.kv_heads;
-    }
+    mine = request(from + (int)(threadIdx.x & 63));
+    units = units_of(mine);
     upto = (uint32_t)wave_upto((int)units);
     all = __builtin_amdgcn_readlane(upto, 63);
   }
   __device__ __forceinline__ void count() {
-    for (int from = 0; from < a.requests; from += 64) {
-      load(from);
-      total += all;
+    if (a.requests <= 64) {
+      load(0);
+      total = all;
+      return;
     }
-    if (a.requests > 64) load(0);
-    before = 0;
+    const int lane = threadIdx.x & 63;
+    uint32_t sum = 0;
+    for (int j = 0; j < a.requests; j += 256) {      // (four requests a lane in flight)
+      PagedRequest r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = request(j + 64 * i + lane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t n = (uint32_t)wave_sum((int)units_of(r[i]));
+        total += n;
+        if (lane == (j >> 6) + i) sum = n;
+      }
+    }
+    chunks_upto = (uint32_t)wave_upto((int)sum);
   }
   // where workgroup p's run begins
   __device__ __forceinline__ uint32_t cut(int p, int log_groups) const { return (uint32_t)((uint64_t)p * total >> log_groups); }
   // log2 of the workgroups that have work: at least a unit each
-  __device__ __forceinline__ int groups() const {
-    return min(a.log_groups, 31 - __clz((int)max(total, 1u)));
-  }
+  __device__ __forceinline__ int groups() const { return min(a.log_groups, 31 - __clz((int)max(total, 1u))); }
   struct Tile { int b, head, row0, unit, n_units; uint32_t first; PagedRequest r; bool there; };      // first: the tile's first unit in the line
+  // the p-th tile, where a unit is one; of more than 64 requests the tile at place p, which takes fewer looks at their lengths
+  __device__ __forceinline__ Tile whole(int p) {
+    Tile t{};
+    if (a.requests <= 64) {
+      load(0);
+      if ((uint32_t)p >= all) return t;
+      return find((uint32_t)p);
+    }
+    const int at = p / a.kv_heads;
+    t.head = p - at * a.kv_heads;
+    t.b = paged_find(a, at, NT == 1 ? 4 : 5);
+    t.there = t.b >= 0;
+    if (!t.there) return t;
+    t.r = paged_request(a, t.b);
+    t.row0 = (at - paged_place(a, t.b, NT == 1 ? 4 : 5)) * 16 * NT;
+    t.there = t.row0 < t.r.fresh * a.share && t.r.fresh * a.share <= a.few_rows;
+    t.n_units = 1;
+    return t;
+  }
   __device__ __forceinline__ Tile find(uint32_t unit) {
-    while (unit >= before + all && base + 64 < a.requests) {
-      before += all;
-      load(base + 64);
+    if (a.requests > 64) {
+      const int chunk = __popcll(__ballot(chunks_upto <= unit));
+      if (chunk < 64) {
+        before = chunk ? __builtin_amdgcn_readlane(chunks_upto, chunk - 1) : 0;
+        if (base != 64 * chunk) load(64 * chunk);
+      } else {      // behind the first 4096 requests: one chunk behind the other
+        if (base < 4096) {
+          before = __builtin_amdgcn_readlane(chunks_upto, 63);
+          load(4096);
+        }
+        while (unit >= before + all && base + 64 < a.requests) {
+          before += all;
+          load(base + 64);
+        }
+      }
     }
     const uint64_t behind = __ballot(before + upto <= unit);
     const int lane = min(63, (int)__popcll(behind));
@@ -96,7 +138,7 @@ template <int D, int NT, int W> struct FewLds {
   float ms[W][M], ls[W][M];
 };
 
-// Workgroup p of 1 << log_groups (of as many as there are tiles where log_groups is -1).
+// Workgroup p of 1 << log_groups (of as many as there are places for tiles where log_groups is -1).
 template <typename T, int D, int NT, int W> __device__ __forceinline__ void paged_few(const PagedArgs& a, FewLds<D, NT, W>& lds, int p) {
   constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 32 * W, C = D / 8, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 32 rows
   constexpr int OP = FewLds<D, NT, W>::OP;
@@ -110,12 +152,9 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
   auto& ls = lds.ls;
 
   FewLine<NT> line(a);
-  line.count();
-  uint32_t u0, u1;
-  if (a.log_groups < 0) {      // a unit is a tile, a workgroup has one
-    u0 = p; u1 = p + 1;
-    if (u0 >= line.total) return;
-  } else {
+  uint32_t u0 = 0, u1 = 1;
+  if (a.log_groups >= 0) {
+    line.count();
     const int log_groups = line.groups();
     if (p >> log_groups) return;
     u0 = line.cut(p, log_groups); u1 = line.cut(p + 1, log_groups);
@@ -124,7 +163,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
   const int in_block = (1 << a.cache.shift) - 1;
 
   for (uint32_t cur = u0; cur < u1;) {
-    const auto tile = line.find(cur);
+    const auto tile = a.log_groups < 0 ? line.whole(p) : line.find(cur);
     if (!tile.there) break;
     const int n = min(tile.n_units - tile.unit, (int)(u1 - cur));
     const PagedRequest r = tile.r;
@@ -355,9 +394,9 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
   }
 }
 
-template <typename T, int D, int NT> __global__ __launch_bounds__(64 * kFewWaves, 2) void paged_few_kernel(const PagedArgs a) {
-  __shared__ __align__(1024) FewLds<D, NT, kFewWaves> lds;
-  paged_few<T, D, NT, kFewWaves>(a, lds, blockIdx.x);
+template <typename T, int D, int NT, int W> __global__ __launch_bounds__(64 * W, 2) void paged_few_kernel(const PagedArgs a) {
+  __shared__ __align__(1024) FewLds<D, NT, W> lds;
+  paged_few<T, D, NT, W>(a, lds, blockIdx.x);
 }
 
 // The parts of a tile: running maximum, sum and 4 results of a thread, N parts requested at a time.
@@ -434,7 +473,10 @@ template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT
 }
 
 template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((paged_few_kernel<T, D, NT>), dim3(a.few_grid), dim3(64 * kFewWaves), 0, s, a);
+  // eight wavefronts fill a CU; whole tiles for more than every CU are done by four each, whose first loads pass while others work (D 128,
+  // 32 / 8 heads: 32 requests of 500 keys 13.5 and 14.0 us, 64 27.3 and 23.8, 256 117 and 89; D 64, 256 of 100 50 and 21)
+  if (a.log_groups < 0 && a.few_grid > 256) hipLaunchKernelGGL((paged_few_kernel<T, D, NT, 4>), dim3(a.few_grid), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged_few_kernel<T, D, NT, 8>), dim3(a.few_grid), dim3(512), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.log_groups < 0) return e;
   hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3(a.few_grid - 1), dim3(FewJoin<D, NT>::kThreads), 0, s, a);

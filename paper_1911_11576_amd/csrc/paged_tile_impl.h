@@ -134,24 +134,16 @@ struct TileLine {
     fill(t, lane, lane);
     return true;
   }
-  // more than 64 requests: their tiles in the order of the rows, no one split.  Request b's begin at place first * share / 128 + b (there are
-  // as many places as it can have tiles, whatever the lengths).
+  // more than 64 requests: their tiles in the order of the rows, no one split
   __device__ __forceinline__ bool find_in_order(int k, TileWork* t) {
-    const int lane = threadIdx.x & 63, slot = a.slots - 1 - k / a.kv_heads;
-    auto begin = [&](int b) { return (int)((int64_t)min(max(a.starts[b], 0), a.tokens) * a.share >> 7) + b; };
-    int n = 0;
-    for (int b0 = 0; b0 < a.requests; b0 += 64) {
-      const int here = __popcll(__ballot(b0 + lane < a.requests && begin(b0 + lane) <= slot));
-      n += here;
-      if (here < 64) break;
-    }
-    if (n == 0) return false;
-    take(n - 1);      // (the same in all lanes)
-    t->tile = slot - begin(n - 1);
+    const int at = a.slots - 1 - k / a.kv_heads, b = paged_find(a, at, 7);
+    if (b < 0) return false;
+    take(b);      // (the same in all lanes)
+    t->tile = at - paged_place(a, b, 7);
     if (t->tile >= __builtin_amdgcn_readfirstlane(tiles)) return false;
     t->parts = 1; t->part = 0; t->partial = 0;
     t->head = k % a.kv_heads;
-    fill(t, 0, n - 1);
+    fill(t, 0, b);
     return true;
   }
 };
