@@ -20,15 +20,21 @@ struct PagedArgs {
   CacheLayout cache;
   int requests, tokens, q_heads, kv_heads, share, width, causal, window;
   float scale2;                    // scale times log2 e: scores are kept in units of log 2
-  int unit_keys;                   // few rows: keys of a unit of work, a multiple of 256
+  int unit_keys;                   // few rows: keys of a unit of work, a multiple of 32 to a wavefront
   int log_groups, few_grid;        // few rows: workgroups, 1 << log_groups of them; log_groups -1: a unit each, which is a whole tile
   int few_rows;                    // requests of up to so many rows are the few-rows kernel's, the others the tile kernel's
   float* tile_partial;             // tiles of 128 rows: up to 2 * kTileShares of [128 * (D + 2)]
-  int slots, least_steps;          // places for tiles; steps of 64 keys that a tile may have in any case before it is split
+  int slots;                       // places for tiles in the order of the rows
 };
 
 // Workgroups of the tile kernel that the chip holds, two to a CU: what is shared out evenly.
 constexpr int kTileShares = 512;
+// A tile is not split into parts of fewer steps of 64 keys (D 128, 32 / 8 heads, 128 tokens behind 1920: 26.6 us with 4, 28.9 with 8, 37.5 with
+// 16; twice 64 behind 4032: 32.9, 30.0, 37.9; 512 and 256 behind 512 and 1792: 44.6, 44.1, 42.7).
+constexpr int kLeastSteps = 8;
+// Requests among which those of many rows are looked for, two times 256 (one of 512 tokens behind 32256 keys and 100 of one behind 4095: 772 us with
+// tiles in the order of the rows, 500 with a line of them; for 1000 single tokens and 20 chunks, where nothing needs it, the looks cost 1283 -> 1320).
+constexpr int kTileRequests = 512;
 
 // A request as the kernels see it: its first row of q, its new tokens, its keys.
 struct PagedRequest { int first, fresh, keys; };

@@ -1,9 +1,10 @@
 // Attention over a paged cache, many rows a request (chunks of prompts): bound by the matrix unit and the exponentials.
 //
 // A workgroup has 128 rows of one request and key head, 32 to a wavefront, and walks the keys that they see 64 at a time: keys
-// and values go through registers into LDS, the next 64 in flight and written to the other half while these are worked on, one
-// barrier a step.  Both dots are v_mfma_f32_32x32x16.  Where there are few tiles their keys are split over workgroups too, and
-// paged_tile_join_kernel adds the parts in the order of the keys.
+// and values by direct loads into LDS, the next 64 in flight to the other half while these are worked on, one
+// barrier a step.  Both dots are v_mfma_f32_32x32x16.  A tile of more than an even share of the work is split over workgroups
+// by its keys, and paged_mixed_join_kernel adds the parts in their order.  905 TFLOP/s at D 128 (8 chunks of 1 to 1024 tokens behind up to 12000 keys, 32 / 8
+// heads, 367 us; the card's rate of a bf16 product of 8192^3 is 1205), 585 at D 64 (4 prompts of 2048 x 16 heads, 58.8 us).
 #pragma once
 #include <algorithm>
 
@@ -29,29 +30,63 @@ template <class Op> __device__ __forceinline__ float halves_allreduce(float v) {
 
 // What a workgroup of the tile kernel has: a tile of 128 rows, all of its keys or a part of them.
 struct TileWork {
-  int b, head, tile;
+  int lane, b, head, tile;      // the lane that has the request (of a line), the request
   PagedRequest r;
   int rows, row0, key_first, steps;      // of the request, of the tile: steps of 64 keys
   int parts, part, partial;              // parts that the keys are split into, this one, and its place among the partial results
 };
 
-// The order of the work, made by every wavefront for itself from the lengths on the device, up to 64 requests one to a lane.  A tile's
+// The order of the work, made by every wavefront for itself from the lengths on the device, up to 64 requests of many rows one to a lane.  A tile's
 // time goes with its steps, which differ up to the whole length of the longest request, and workgroups start in order as others end.
-// So: the tiles of more steps than an even share of all (a 512th) are split into parts of at most that and come first; the
+// So: the tiles of more steps than an even share of all work, that of few rows with it (63 requests of one token behind 2000 keys and one
+// of 1000: 125 us, 155 where shares are of the tiles alone), are split into parts of at most that and come first; the
 // others follow by falling steps.  Steps do not fall along a request's tiles, so how many of them have at least s is a
 // formula, and the k-th tile is found by bisection over s.  (Chunks of 1 to 1024 tokens behind contexts of up to 12000: the longest tile alone is 1.2
-// times the even share; request by request the launch took 1.48 times it.)
+// times the even share; request by request the launch took 1.48 times it.)  A share is 1.25 times a 512th, so that parts of one length do
+// not come out one more than places (512 tokens behind 7680: 99 us, 116 with 1.5, which makes 384 parts; 32768: 319 and 379).
 struct TileLine {
   const PagedArgs& a;
   PagedRequest mine{};
+  int id = 0;                                // the lane's request
   int tiles = 0, flat = -1;      // of the lane's request; with a window, or without the causal mask: steps of each of its tiles, as good as equal
   int share_steps = 0;           // an even share
   int split = 0, parts = 1;      // the lane's tiles of more steps than that (its last ones), and the parts of each
   int items = 0;                 // parts of all
+  int others = 0;                // steps of requests of few rows that the lane looked at, in 64s
 
   __device__ __forceinline__ explicit TileLine(const PagedArgs& args) : a(args) {}
-  __device__ __forceinline__ void take(int b) {
-    mine = b < a.requests ? paged_request(a, b) : PagedRequest{};
+  __device__ __forceinline__ PagedRequest request(int b) const { return b < a.requests ? paged_request(a, b) : PagedRequest{}; }
+  // those of many rows among up to kTileRequests, one a lane; false: there are more than 64
+  __device__ __forceinline__ bool gather() {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int b0 = 0; b0 < a.requests; b0 += 256) {
+      PagedRequest r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) r[i] = request(b0 + 64 * i + lane);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        look(r[i]);
+        const uint64_t many = __ballot(r[i].fresh * a.share > a.few_rows), below = (1ull << lane) - 1;
+        if (!many) continue;
+        const int here = __popcll(many);
+        if (n + here > 64) return false;
+        // the lanes that have one go behind those that are there, the others behind them
+        const int to = n + (many >> lane & 1 ? __popcll(many & below) : here + __popcll(~many & below)) & 63;
+        const int b = __builtin_amdgcn_ds_permute(4 * to, b0 + 64 * i + lane), first = __builtin_amdgcn_ds_permute(4 * to, r[i].first);
+        const int fresh = __builtin_amdgcn_ds_permute(4 * to, r[i].fresh), keys = __builtin_amdgcn_ds_permute(4 * to, r[i].keys);
+        if (lane >= n && lane < n + here) { id = b; mine = PagedRequest{first, fresh, keys}; }
+        n += here;
+      }
+    }
+    return true;
+  }
+  // 64 keys of a tile of few rows, which memory bounds, take a place on a CU as long as a step of 128 rows
+  __device__ __forceinline__ void look(const PagedRequest& r) {
+    const int rows = r.fresh * a.share;
+    if (rows > 0 && rows <= a.few_rows) others = (int)min((int64_t)others + ((int64_t)((r.keys - paged_first_key(a, r) + 63) >> 6) * a.kv_heads >> 6), (int64_t)1 << 24);
+  }
+  __device__ __forceinline__ void measure() {
     const int rows = mine.fresh * a.share;
     tiles = rows > a.few_rows ? (rows + 127) >> 7 : 0;
     flat = -1;
@@ -66,17 +101,25 @@ struct TileLine {
     return token >= mine.fresh ? 0 : tiles - (max(token, 0) * a.share >> 7);
   }
   __device__ __forceinline__ int last_steps() const { return tiles == 0 ? 0 : flat >= 0 ? flat : (mine.keys + 63) >> 6; }
-  __device__ __forceinline__ void order() {
-    take(threadIdx.x & 63);
+  // false: more than 64 requests of many rows, or of any more than the line looks at
+  __device__ __forceinline__ bool order() {
+    if (a.requests <= 64) {
+      id = threadIdx.x & 63;
+      mine = request(id);
+      look(mine);
+    } else if (a.requests > kTileRequests || !gather()) {
+      return false;
+    }
+    measure();
     const int last = last_steps(), first = flat >= 0 || tiles == 0 ? last : max(0, mine.keys - mine.fresh + 64) >> 6;
     // (in 64 steps: no more than 2^31 of them)
-    const int total = wave_sum((int)min((int64_t)tiles * (first + last) * a.kv_heads >> 7, (int64_t)1 << 24));
-    share_steps = min(1 << 23, max(a.least_steps, (total + total / 4) / (kTileShares / 64)));      // (a tile has up to 2^24)
+    const int total = wave_sum((int)min(others + ((int64_t)tiles * (first + last) * a.kv_heads >> 7), (int64_t)1 << 24));
+    share_steps = min(1 << 23, max(kLeastSteps, (total + total / 4) / (kTileShares / 64)));      // (a tile has up to 2^24)
     for (;; share_steps *= 2) {      // (never more parts than there is room for)
       split = at_least(share_steps + 1);
       parts = split ? (last + share_steps - 1) / share_steps : 1;
       items = wave_sum((int)min((int64_t)split * parts * a.kv_heads, (int64_t)1 << 24));
-      if (items <= 2 * kTileShares) return;
+      if (items <= 2 * kTileShares) return true;
     }
   }
   // the lane among whose `count` the number k falls, k counted from there on
@@ -86,8 +129,9 @@ struct TileLine {
     *k -= __builtin_amdgcn_readlane(upto, lane) - __builtin_amdgcn_readlane(count, lane);
     return lane;
   }
-  __device__ __forceinline__ void fill(TileWork* t, int lane, int b) const {
-    t->b = b;
+  __device__ __forceinline__ void fill(TileWork* t, int lane) const {
+    t->lane = lane;
+    t->b = __builtin_amdgcn_readlane(id, lane);
     t->r = PagedRequest{__builtin_amdgcn_readlane(mine.first, lane), __builtin_amdgcn_readlane(mine.fresh, lane), __builtin_amdgcn_readlane(mine.keys, lane)};
     t->rows = t->r.fresh * a.share;
     t->row0 = t->tile * 128;
@@ -113,37 +157,42 @@ struct TileLine {
       before = wave_sum((int)(threadIdx.x & 63) < lane ? all : 0);
     }
     t->partial = whole ? before + at : k;
-    fill(t, lane, lane);
+    fill(t, lane);
   }
   // the places of a tile's parts among the partial results are so far apart
-  __device__ __forceinline__ int stride(const TileWork& t) const { return __builtin_amdgcn_readlane(split, t.b) * a.kv_heads; }
+  __device__ __forceinline__ int stride(const TileWork& t) const { return __builtin_amdgcn_readlane(split, t.lane) * a.kv_heads; }
   // the k-th of the tiles that are not split, by falling steps; false: there are not so many
   __device__ __forceinline__ bool find_whole(int k, TileWork* t) const {
     if (k >= wave_sum(tiles - split) * a.kv_heads) return false;
-    int lo = 0, hi = share_steps + 1;      // more than k of at least lo steps, no more than k of at least hi
+    // in eighths of an even share: tiles of about the same steps go request by request, whose keys the L2s then have (20 requests of 400
+    // rows x 32 heads behind 3600 keys: 620 us, in the order of single steps 690)
+    const int grain = max(1, share_steps >> 3);
+    int lo = 0, hi = share_steps / grain + 1;      // more than k of at least lo eighths, no more than k of at least hi
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if (wave_sum(at_least(mid) - split) * a.kv_heads > k) lo = mid; else hi = mid;
+      if (wave_sum(max(0, at_least(mid * grain) - split)) * a.kv_heads > k) lo = mid; else hi = mid;
     }
-    const int more = at_least(hi) - split, here = at_least(lo) - split - more;
+    const int more = max(0, at_least(hi * grain) - split), here = at_least(lo * grain) - split - more;
     k -= wave_sum(more) * a.kv_heads;
     const int lane = among(here * a.kv_heads, &k);
     t->parts = 1; t->part = 0; t->partial = 0;
     t->head = k % a.kv_heads;
-    t->tile = __builtin_amdgcn_readlane(tiles - split - more - here, lane) + k / a.kv_heads;
-    fill(t, lane, lane);
+    t->tile = __builtin_amdgcn_readlane(tiles - split - more, lane) - 1 - k / a.kv_heads;
+    fill(t, lane);
     return true;
   }
-  // more than 64 requests: their tiles in the order of the rows, no one split
+  // without a line: the tiles in the order of the rows, no one split
   __device__ __forceinline__ bool find_in_order(int k, TileWork* t) {
     const int at = a.slots - 1 - k / a.kv_heads, b = paged_find(a, at, 7);
     if (b < 0) return false;
-    take(b);      // (the same in all lanes)
+    id = b;      // (the same in all lanes)
+    mine = request(b);
+    measure();
     t->tile = at - paged_place(a, b, 7);
     if (t->tile >= __builtin_amdgcn_readfirstlane(tiles)) return false;
     t->parts = 1; t->part = 0; t->partial = 0;
     t->head = k % a.kv_heads;
-    fill(t, 0, b);
+    fill(t, 0);
     return true;
   }
 };
@@ -172,10 +221,9 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile(const Pa
   TileWork work;
   {
     TileLine line(a);
-    if (a.requests > 64) {
+    if (!line.order()) {
       if (!line.find_in_order(k, &work)) return;
     } else {
-      line.order();
       if (k < line.items) line.find_split(k, false, &work);
       else {
         // by turns forwards and backwards over 256 places, eight by eight (one to an XCD), so that what the CUs get one after the other adds up to
@@ -418,7 +466,7 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile(const Pa
 // Tiles whose keys were split: workgroup b of `groups` joins every groups-th run of 4096 values of them, the parts in the order of the keys.
 template <typename T, int D> __device__ __forceinline__ void paged_tile_join(const PagedArgs& a, int b, int groups) {
   TileLine line(a);
-  line.order();
+  if (!line.order()) return;
   const int runs = wave_sum(line.split) * a.kv_heads * (D / 32);
   for (; b < runs; b += groups) {
     const int k = b / (D / 32), run = b - k * (D / 32);
@@ -466,7 +514,7 @@ template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT
 }
 
 template <typename T, int D, int NT> hipError_t paged_mixed_launch(const PagedArgs& a, hipStream_t s) {
-  const bool ordered = a.requests <= 64;
+  const bool ordered = a.requests <= kTileRequests;
   const int tiles = std::max(a.few_grid, a.slots * a.kv_heads + (ordered ? 2 * kTileShares : 0));
   hipLaunchKernelGGL((paged_mixed_kernel<T, D, NT>), dim3((unsigned)(a.few_grid + tiles)), dim3(256), 0, s, a);
   const hipError_t e = hipGetLastError();

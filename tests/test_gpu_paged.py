@@ -389,6 +389,20 @@ def test_attention_of_many_requests(q_heads, kv_heads, requests):
     check_attention(c, window=2**31 - 1)
 
 
+@pytest.mark.parametrize("requests, chunks", [(64, 3), (65, 3), (130, 64), (130, 65), (300, 1), (512, 5), (513, 5)])
+def test_attention_of_chunks_among_many_requests(requests, chunks):
+    """A few long chunks, whose keys are split, scattered among single tokens; as many chunks as one line takes, and one more."""
+    rng = np.random.default_rng(requests + chunks)
+    new, keys = rng.integers(0, 3, requests), rng.integers(3, 40, requests)
+    for b in rng.permutation(requests)[:chunks]:
+        new[b] = rng.integers(5, 70)
+        keys[b] = rng.integers(new[b], 2500 if chunks < 10 else 300)
+    c = problem(rng, "f16", [int(k) for k in keys], [int(n) for n in new], 8, 2, 64, 16)
+    check_attention(c)
+    check_attention(c, window=500)
+    check_attention(c, causal=False)
+
+
 @pytest.mark.parametrize("new", [1, 2, 60])
 def test_attention_of_one_long_request(new):
     """Keys of one tile over many workgroups: the parts are joined in the order of the keys."""
