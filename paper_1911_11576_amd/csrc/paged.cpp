@@ -182,6 +182,7 @@ fs_status fs_plan_create_rotary(const fs_rotary_desc* desc, fs_plan** out) {
     s.units = (int)((dim + 2 * w - 1) / (2 * w));
     s.heads = d.q_heads + d.k_heads * (store ? 2 : 1);
     fs::rotary_geometry(&s);
+    if (w == 8 && s.heads_each > 1) p->lds_bytes = 8ll * s.most_angles;
     const int64_t q_row = d.q_heads * dim, k_row = d.k_heads * dim;
     fs::PagedPlan& g = p->paged;
     g.kind = FS_SCHED_ROTARY;

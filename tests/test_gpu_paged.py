@@ -187,6 +187,50 @@ def test_rotary_store(dtype, tokens, q_heads, k_heads, dim, rot, block_size, ord
         within(f64(cache), paged.stored(empty, rows, slots), paged.stored(0 * empty, bound, slots), "cache")
 
 
+@pytest.mark.parametrize("dtype, heads, dim, rot, interleaved, store", [
+    ("f16", 72, 64, 32, False, True), ("bf16", 72, 64, 64, False, False), ("f16", 24, 128, 96, False, False), ("bf16", 36, 128, 128, False, True), ("bf16", 60, 96, 32, False, True),
+    ("f16", 99, 32, 16, False, False), ("bf16", 48, 64, 32, True, True), ("f32", 45, 64, 48, True, False), ("f32", 21, 128, 64, False, True), ("bf16", 3, 256, 64, False, False),
+    ("f16", 3, 512, 512, False, True)])
+def test_rotary_of_many_rows(dtype, heads, dim, rot, interleaved, store):
+    """Enough rows that threads have several heads: with angles of their own and of a workgroup's, one vector of a head and two, in place too."""
+    width = 4 if dtype == "f32" else 8
+    tokens = -(-4 * 131072 * 2 * width // (dim * heads)) + 1
+    rng, g = np.random.default_rng(dim + heads), torch.Generator("cuda").manual_seed(heads)
+    k_heads = heads // 3
+    x = [torch.randn((tokens, h, dim), device="cuda", generator=g).to(DT[dtype]) for h in (heads - k_heads * (1 + store), *([k_heads] * (1 + store)))]
+    freqs, pos = fs_rotary_frequencies(rot), positions_of(rng, tokens, 1 << 20)
+    frq, p = torch.tensor(freqs, dtype=torch.float64, device="cuda"), i32(pos)
+    kw = dict(interleaved=interleaved, inverse=not store, magnitude=1.25)
+    want = [paged.rotary(f64(t), pos, freqs, interleaved, not store, 1.25) for t in x[:2]]
+    room = [rotary_bound(f64(t), w, freqs, interleaved, 1.25, dtype) for t, w in zip(x, want)]
+    if not store:
+        with Plan.rotary(dtype, tokens, x[0].shape[1], k_heads, dim, rot, **kw) as plan:
+            outs = [torch.full_like(t, float("nan")) for t in x]
+            plan.launch([*x, p, frq], outs)
+            for o, w, b in zip(outs, want, room):
+                within(f64(o), w, b, "rotary")
+            plan.launch([*x, p, frq], x)
+            assert all(torch.equal(a, b) for a, b in zip(x, outs))
+        return
+    blocks = -(-tokens // 16) + 2
+    slots = rng.permutation(blocks * 16)[:tokens]
+    padding = rng.random(tokens) < 0.1
+    slots[padding] = -1
+    caches = [torch.full((blocks, k_heads, 16, dim), 7.0, dtype=DT[dtype], device="cuda") for _ in range(2)]
+    q_out = torch.full_like(x[0], 5.0)
+    with Plan.rotary(dtype, tokens, x[0].shape[1], k_heads, dim, rot, blocks=blocks, block_size=16, **kw) as plan:
+        plan.launch([*x, p, frq, i32(slots)], [q_out, *caches])
+        want[0][padding], room[0][padding] = 5.0, 0
+        within(f64(q_out), want[0], room[0], "q")
+        empty = np.full((blocks, k_heads, 16, dim), 7.0)
+        within(f64(caches[0]), paged.stored(empty, want[1], slots), paged.stored(0 * empty, room[1], slots), "k")
+        assert np.array_equal(f64(caches[1]), paged.stored(empty, f64(x[2]), slots))
+        same = x[0].clone()      # in place: padding rows stay as they are
+        plan.launch([same, *x[1:], p, frq, i32(slots)], [same, *caches])
+        keep = torch.tensor(padding, device="cuda")
+        assert torch.equal(same[~keep], q_out[~keep]) and torch.equal(same[keep], x[0][keep])
+
+
 def test_rotary_gradient():
     """Against the formula's own (the transpose) and against differences, through torch's autograd."""
     t, h, d = 6, 2, 32
