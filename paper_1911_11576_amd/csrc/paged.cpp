@@ -104,8 +104,9 @@ fs_status fs_plan_create_block_tables(const fs_block_tables_desc* desc, fs_plan*
     if (!blocks_fit(d.blocks, d.block_size, &shift, err) || !blocks_fit(d.table_blocks, d.block_size, &shift, err)) return false;
     fs::BlockTablesSpec& s = p->paged.tables;
     s.d = d;
-    // Every workgroup scans all requests for itself and serves a row a thread.  One wavefront for a decode step; else a thread a
-    // request where a workgroup has so many (515 requests, 32768 rows: 5.7 us with three requests and two rows to one of 256 threads).
+    // Every workgroup scans all requests for itself and serves a row a thread.  One wavefront for a decode step (the kernel of 48 requests
+    // 2.2 us, of 256 threads 2.4); else a thread a request, in as small a workgroup as has so many (256 requests, 32768 rows: 3.5 us, of 1024
+    // threads 4.5; 515 requests: 4.6, of 256 threads, with three requests and two rows each, 5.7), and beyond 1024 four.
     s.wg = d.requests <= 64 && d.tokens <= 64 ? 64 : d.requests <= 256 ? 256 : 1024;
     s.grid = (int)std::min<int64_t>(std::max<int64_t>(1, ((int64_t)d.tokens + s.wg - 1) / s.wg), 2048);
     s.lds = 12ll * (d.requests + 1) + 64;

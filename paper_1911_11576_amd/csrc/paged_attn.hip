@@ -44,7 +44,8 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   *lds_bytes = std::max<int64_t>(waves * 128 * d.head_dim, waves * m * (d.head_dim + 4) * 4) + waves * (512 + 8 * m);
   if (many) {
     s->slots = ((int64_t)d.tokens * s->share >> 7) + d.requests;
-    if (s->slots * d.kv_heads > 0x7ffff000ll) { *err = "too many tiles for one grid"; return false; }
+    if (s->slots * d.kv_heads > (1 << 24) - 2048) {      // (a grid has less than 2^32 threads)
+      *err = "too many tiles for one grid"; return false; }
     if (any && d.requests <= kTileRequests) s->partial_bytes += 2ll * kTileShares * 128 * (d.head_dim + 2) * 4;
     *lds_bytes = std::max<int64_t>(*lds_bytes, 512 * d.head_dim + 48);
   }

@@ -447,6 +447,24 @@ def test_attention_of_chunks_among_many_requests(requests, chunks):
     check_attention(c, causal=False)
 
 
+@pytest.mark.parametrize("table_keys, long", [(64, 60), (2048, 1900)])
+def test_attention_of_thousands_of_requests(table_keys, long):
+    """More than 4096 requests, single tokens: a workgroup each tile, and equal runs whose ends are searched behind the first 4096."""
+    requests = 4300
+    rng = np.random.default_rng(table_keys)
+    lengths = rng.integers(0, 4, requests)
+    new = np.minimum(lengths, rng.integers(0, 2, requests))
+    for b in (0, 63, 64, 4095, 4096, 4200, 4299):
+        lengths[b], new[b] = long - b % 7, 1
+    blocks, size, dim, heads = 600, 16, 32, 2
+    g = torch.Generator("cuda").manual_seed(5)
+    caches = [torch.randn((blocks, 1, size, dim), device="cuda", generator=g).half() for _ in range(2)]
+    tables = rng.integers(0, blocks, (requests, table_keys // size))
+    c = dict(dtype="f16", q=torch.randn((int(new.sum()) + 1, heads, dim), device="cuda", generator=g).half(), caches=caches, tables=tables, lengths=lengths,
+             starts=np.concatenate([[0], np.cumsum(new)]), order="head", block_size=size, kv_heads=1, scale=dim ** -0.5)
+    check_attention(c, max_new=1)
+
+
 @pytest.mark.parametrize("new", [1, 2, 60])
 def test_attention_of_one_long_request(new):
     """Keys of one tile over many workgroups: the parts are joined in the order of the keys."""

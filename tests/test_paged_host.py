@@ -58,6 +58,13 @@ def test_attention_unsupported(change, text):
     refused(Plan.paged_attention, binding.FS_ERR_UNSUPPORTED, text, **dict(ATTENTION, **change))
 
 
+def test_attention_of_more_tiles_than_a_grid_has():
+    """Tiles of 128 rows: tokens * share / 128 + requests places for every key head, 256 threads each, below 2^32 of them."""
+    change = dict(requests=32760, tokens=100, q_heads=512, kv_heads=512, max_new=0)
+    Plan.paged_attention(**dict(ATTENTION, **change))[0].close()
+    refused(Plan.paged_attention, binding.FS_ERR_UNSUPPORTED, "too many tiles", **dict(ATTENTION, **dict(change, requests=32768)))
+
+
 def test_null_arguments():
     L, out, n = binding.lib(), C.c_void_p(), C.c_int64()
     assert L.fs_plan_create_block_tables(None, C.byref(out)) == binding.FS_ERR_INVALID
