@@ -7,7 +7,7 @@
 // wavefronts' maxima, sums and results meet in LDS; a tile that one workgroup does from end to end is stored, parts of others go to
 // the partial results, which paged_few_join_kernel adds in the order of the keys.  Where no request can be long a workgroup has
 // one tile and all of its keys, and nothing is left to join.  6.2 TB/s for 64 requests of one token behind up to 24000 keys (32 / 8 heads of 128, 360 us; a copy of
-// 1 GiB reaches 6.6), 5.4 for one behind 131072 (99 us, 7 of them the second kernel); keys and values through the caches 397 and 108.
+// 1 GiB reaches 6.6), 5.5 for one behind 131072 (97 us); keys and values through the caches 397 and 108.
 #pragma once
 #include "paged_attn_impl.h"
 
@@ -423,46 +423,55 @@ template <int N, int M, int D, class Part> __device__ __forceinline__ void few_a
   for (int i = 0; i < N; ++i) few_add(s, m[i], l[i], o[i]);
 }
 
-// Tiles that several workgroups did: the workgroup that stands at the first cut p inside one joins its parts, in the order of
-// the keys.  A wavefront has 256 values of it; up to 16 wavefronts, which take turns with the parts where the values are fewer.
-template <int D, int NT> struct FewJoin { static constexpr int kRuns = 16 * NT * D / 256, kTurns = kRuns > 8 ? 1 : 16 / kRuns, kThreads = 64 * kRuns * kTurns; };
-template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_join(const PagedArgs& a, int p) {
-  constexpr int M = 16 * NT, R = FewJoin<D, NT>::kRuns, W = FewJoin<D, NT>::kTurns;
+// Tiles that several workgroups did, their parts added in the order of the keys: there is a workgroup here for every cut p of the line, and
+// those whose cuts lie in one tile share its rows, 256 values to a run.  A wavefront has a run, or takes turns with others at its parts where the
+// runs are fewer (one token behind 131072 keys, 32 parts to a tile: 96.7 us with the first kernel, 99.2 where the workgroup
+// of the first cut does all runs).
+template <int D, int NT> struct FewJoin { static constexpr int kRuns = 16 * NT * D / 256, kWaves = kRuns > 8 ? kRuns : 16 / kRuns * kRuns, kThreads = 64 * kWaves; };
+template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_join(const PagedArgs& a, FewLine<NT>& line, int log_groups, int p) {
+  constexpr int M = 16 * NT, R = FewJoin<D, NT>::kRuns, W = FewJoin<D, NT>::kWaves;
   constexpr int64_t kFloats = FewPart<D, NT>::kFloats;
-  __shared__ FewSum sums[R * W][64];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), w = wave / R, run = wave - w * R;
-  FewLine<NT> line(a);
-  line.count();
-  const int log_groups = line.groups();
-  if (p >> log_groups) return;
+  __shared__ FewSum sums[W][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const uint32_t at = line.cut(p, log_groups);
-  if (at >= line.total) return;
+  if (p >> log_groups || at >= line.total) return;
   const auto tile = line.find(at);
-  const uint32_t first = tile.first, end = first + tile.n_units, before = line.cut(p - 1, log_groups);
-  if (!tile.there || at == first || before > first) return;      // no part before the cut, or another cut is the first
-  int last = p;                                   // the workgroup that the last part is of
-  while (last + 1 < 1 << log_groups && line.cut(last + 1, log_groups) < end) ++last;
+  const uint32_t first = tile.first, end = first + tile.n_units;
+  if (!tile.there || at == first) return;      // no part before the cut
+  // the first cut behind the tile's first unit, the last one before its end: p * total / groups > first, < end
+  // (mostly this one is both, which costs no division)
+  auto cut_behind = [&](uint32_t unit) { return (((uint64_t)unit << log_groups) + line.total - 1) / line.total; };
+  const uint64_t cut0 = line.cut(p - 1, log_groups) <= first ? p : cut_behind(first + 1), behind = line.cut(p + 1, log_groups) >= end ? p + 1 : cut_behind(end);
+  if (cut0 < 1 || cut0 > (uint64_t)p || behind <= (uint64_t)p) return;      // (not where rows of several requests are more units than 32 bits number)
+  const int p0 = (int)cut0, last = (int)min(behind, (uint64_t)1 << log_groups) - 1;
+  const int rows = min(M, tile.r.fresh * a.share - tile.row0), runs = (rows * D + 255) / 256;      // runs that have rows
+  const int sharing = min(last - p0 + 1, runs), here = (runs + sharing - 1) / sharing, turns = W / here;
+  if (p - p0 >= sharing) return;
+  const int turn = wave / here, run = (p - p0) * here + wave - turn * here;
+  const bool working = run < runs && turn < turns;
   const int e = run * 256 + lane * 4, row = e / D;
-  const int n = last - p + 2;
-  auto part = [&](int k) { return a.partial + (2 * (p - 1 + k) + (k == 0 && before != first ? 1 : 0)) * kFloats; };
+  const int n = last - p0 + 2;
+  const bool whole = line.cut(p0 - 1, log_groups) == first;      // the first part is the first of its workgroup
+  auto part = [&](int k) { return a.partial + (2 * (p0 - 1 + k) + (k == 0 && !whole ? 1 : 0)) * kFloats; };
   FewSum s{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
-  int k = w;
-  for (; k + 7 * W < n; k += 8 * W) few_add_parts<8, M, D>(s, k, W, part, row, e);
-  if (k + 3 * W < n) { few_add_parts<4, M, D>(s, k, W, part, row, e); k += 4 * W; }
-  if (k + W < n) { few_add_parts<2, M, D>(s, k, W, part, row, e); k += 2 * W; }
-  if (k < n) few_add_parts<1, M, D>(s, k, W, part, row, e);
-  if constexpr (W > 1) {
+  if (working) {
+    int k = turn;
+    for (; k + 7 * turns < n; k += 8 * turns) few_add_parts<8, M, D>(s, k, turns, part, row, e);
+    if (k + 3 * turns < n) { few_add_parts<4, M, D>(s, k, turns, part, row, e); k += 4 * turns; }
+    if (k + turns < n) { few_add_parts<2, M, D>(s, k, turns, part, row, e); k += 2 * turns; }
+    if (k < n) few_add_parts<1, M, D>(s, k, turns, part, row, e);
+  }
+  if (turns > 1) {
     sums[wave][lane] = s;
     __syncthreads();
-    if (w) return;
-#pragma unroll
-    for (int i = 1; i < W; ++i) {
-      const FewSum& x = sums[i * R + run][lane];
+    if (!working || turn) return;
+    for (int i = 1; i < min(turns, n); ++i) {
+      const FewSum& x = sums[i * here + wave][lane];
       few_add(s, x.m, x.l, x.o);
     }
   }
-  if (tile.row0 + row >= tile.r.fresh * a.share) return;
-  const int token = (tile.row0 + row) / a.share, head = tile.head * a.share + (tile.row0 + row) - token * a.share;
+  if (!working || row >= rows) return;
+  const int r = tile.row0 + row, token = r / a.share, head = tile.head * a.share + r - token * a.share;
   const float inv = s.l == 0.f ? 0.f : 1.f / s.l;
   *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(a.out) + (int64_t)(tile.r.first + token) * a.out_stride + (int64_t)head * D + e % D) =
       u32x2{Mfma<T>::pack(s.o[0] * inv, s.o[1] * inv), Mfma<T>::pack(s.o[2] * inv, s.o[3] * inv)};
@@ -470,7 +479,9 @@ template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_j
 }
 
 template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT>::kThreads)) void paged_few_join_kernel(const PagedArgs a) {
-  paged_few_join<T, D, NT>(a, blockIdx.x + 1);
+  FewLine<NT> line(a);
+  line.count();
+  paged_few_join<T, D, NT>(a, line, line.groups(), blockIdx.x + 1);
 }
 
 template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs& a, hipStream_t s) {

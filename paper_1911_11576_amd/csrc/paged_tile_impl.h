@@ -507,8 +507,12 @@ template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT
     paged_tile_join<T, D>(a, blockIdx.x - 256, 256);
     return;
   }
+  FewLine<NT> line(a);
+  line.count();
+  if (line.total == 0) return;
+  const int log_groups = line.groups();
   for (int p = blockIdx.x + 1; p < a.few_grid; p += 256) {
-    paged_few_join<T, D, NT>(a, p);
+    paged_few_join<T, D, NT>(a, line, log_groups, p);
     __syncthreads();
   }
 }
