@@ -96,8 +96,9 @@ struct TileLine {
   // tiles of the lane's request with at least s steps: a tile's last token t has ceil((keys - fresh + 1 + t) / 64)
   __device__ __forceinline__ int at_least(int s) const {
     if (s <= 0) return tiles;
+    if (s > (1 << 24) + 8) return 0;      // (2^30 keys are no more steps, and s times 64 would leave 32 bits)
     if (flat >= 0) return flat >= s ? tiles : 0;
-    const int token = __builtin_elementwise_sub_sat((s - 1) << 6, mine.keys - mine.fresh);      // the first such token (s is no more than 2^24)
+    const int token = __builtin_elementwise_sub_sat((s - 1) << 6, mine.keys - mine.fresh);      // the first such token
     return token >= mine.fresh ? 0 : tiles - (max(token, 0) * a.share >> 7);
   }
   __device__ __forceinline__ int last_steps() const { return tiles == 0 ? 0 : flat >= 0 ? flat : (mine.keys + 63) >> 6; }

@@ -465,6 +465,24 @@ def test_attention_of_thousands_of_requests(table_keys, long):
     check_attention(c, max_new=1)
 
 
+@pytest.mark.parametrize("new", [1, 3, 90])
+def test_attention_behind_a_billion_keys(new):
+    """2^30 - 5 keys, the most that a row of the table may name but five, of which a window leaves the last ones: as of a request of the same end alone."""
+    rng, g = np.random.default_rng(new), torch.Generator("cuda").manual_seed(new)
+    blocks, size, dim, row, keys = 7, 1024, 64, 1 << 20, 2**30 - 5
+    caches = [torch.randn((blocks, 2, size, dim), device="cuda", generator=g).bfloat16() for _ in range(2)]
+    tables = rng.integers(0, blocks, (2, row))
+    c = dict(dtype="bf16", q=torch.randn((new + 2, 6, dim), device="cuda", generator=g).bfloat16(), caches=caches, tables=tables, lengths=np.array([keys, 40]), starts=np.array([0, new, new + 2]),
+             order="head", block_size=size, kv_heads=2, scale=0.125)
+    end = dict(c, tables=np.where([[True], [False]], tables[:, -3:], tables[:, :3]), lengths=np.array([keys - (row - 3) * size, 40]))
+    plan, nbytes = plan_of(c, 700, max_new=new)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+        torch.cuda.synchronize()
+    check_out(c, outs, wanted(end, 700))
+
+
 @pytest.mark.parametrize("new", [1, 2, 60])
 def test_attention_of_one_long_request(new):
     """Keys of one tile over many workgroups: the parts are joined in the order of the keys."""
