@@ -77,6 +77,8 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.unit_keys = s.unit_keys; a.log_groups = s.log_groups; a.few_grid = s.few_grid;
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.few_rows = s.few_rows;
+  a.log_heads = s.log_groups < 0 ? 0 : std::min(5, __builtin_ctz((unsigned)s.d.kv_heads));
+  a.head_sets = s.d.kv_heads >> a.log_heads;
   if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;
   a.slots = (int)s.slots;
   const bool f16 = s.d.dtype == FS_F16;

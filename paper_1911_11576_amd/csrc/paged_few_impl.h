@@ -1,7 +1,9 @@
 // Attention over a paged cache, few rows a request (single tokens, a few guessed ones): bound by the reading of keys and values.
 //
-// The work of all requests is one line of units, (request, key head, tile of 16 * NT rows, run of keys), cut into as many equal
-// runs as there are workgroups: each finds its own from the lengths on the device, whatever their spread.  A workgroup's
+// The work of all requests is one line of units, (request, set of key heads, tile of 16 * NT rows, run of keys), cut into equal
+// runs, one to as many workgroups as a set has heads: each finds its own from the lengths on the device, whatever their spread.  A set is the largest power of two, up to the
+// 32 CUs of an XCD, that divides the key heads: its workgroups walk the same keys of the heads at the same time behind one L2, which thereby fetches the lines that
+// heads share once (VV).  A workgroup's
 // wavefronts take 32 keys each of a step; a wavefront brings keys and values into LDS of its own by direct loads of whole rows (no
 // barrier in the loop), the next 32 keys as soon as the first dot is through with these, their values behind the second.  At the end of a tile's run the
 // wavefronts' maxima, sums and results meet in LDS; a tile that one workgroup does from end to end is stored, parts of others go to
@@ -17,7 +19,7 @@ namespace fs {
 // Partial results of a workgroup: its first run of a tile and its last, each M rows of D sums, M maxima, M sums of exponentials.
 template <int D, int NT> struct FewPart { static constexpr int kRows = 16 * NT, kFloats = kRows * (D + 2); };
 
-// The line of units.  Every wavefront looks at it for itself, 64 requests at a time, one a lane.
+// The line of units, of one key head of a set.  Every wavefront looks at it for itself, 64 requests at a time, one a lane.
 template <int NT> struct FewLine {
   const PagedArgs& a;
   uint32_t total = 0;
@@ -34,7 +36,7 @@ template <int NT> struct FewLine {
   }
   __device__ __forceinline__ uint32_t units_of(const PagedRequest& r) const {
     if (r.fresh * a.share > a.few_rows) return 0;
-    return (uint32_t)((r.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(r) * (uint32_t)a.kv_heads;
+    return (uint32_t)((r.fresh * a.share + 16 * NT - 1) / (16 * NT)) * (uint32_t)key_units(r) * (uint32_t)a.head_sets;
   }
   __device__ __forceinline__ PagedRequest request(int b) const { return b < a.requests ? paged_request(a, b) : PagedRequest{}; }
   __device__ __forceinline__ void load(int from) {
@@ -67,8 +69,8 @@ template <int NT> struct FewLine {
   }
   // where workgroup p's run begins
   __device__ __forceinline__ uint32_t cut(int p, int log_groups) const { return (uint32_t)((uint64_t)p * total >> log_groups); }
-  // log2 of the workgroups that have work: at least a unit each
-  __device__ __forceinline__ int groups() const { return min(a.log_groups, 31 - __clz((int)max(total, 1u))); }
+  // log2 of the workgroups that have work, of one key head of a set: at least a unit each
+  __device__ __forceinline__ int groups() const { return min(a.log_groups - a.log_heads, 31 - __clz((int)max(total, 1u))); }
   struct Tile { int b, head, row0, unit, n_units; uint32_t first; PagedRequest r; bool there; };      // first: the tile's first unit in the line
   // the p-th tile, where a unit is one; of more than 64 requests the tile at place p, which takes fewer looks at their lengths
   __device__ __forceinline__ Tile whole(int p) {
@@ -78,8 +80,8 @@ template <int NT> struct FewLine {
       if ((uint32_t)p >= all) return t;
       return find((uint32_t)p);
     }
-    const int at = p / a.kv_heads;
-    t.head = p - at * a.kv_heads;
+    const int at = p / a.head_sets;
+    t.head = p - at * a.head_sets;
     t.b = paged_find(a, at, NT == 1 ? 4 : 5);
     t.there = t.b >= 0;
     if (!t.there) return t;
@@ -119,7 +121,7 @@ template <int NT> struct FewLine {
     t.head = tiles ? (int)(tile / tiles) : 0;
     t.row0 = (int)(tile - t.head * tiles) * 16 * NT;
     // (requests whose rows overlap can be more units than 32 bits number: then what was found may be no tile)
-    t.there = t.b < a.requests && (unsigned)t.head < (unsigned)a.kv_heads && t.row0 >= 0 && t.row0 < t.r.fresh * a.share;
+    t.there = t.b < a.requests && (unsigned)t.head < (unsigned)a.head_sets && t.row0 >= 0 && t.row0 < t.r.fresh * a.share;
     return t;
   }
 };
@@ -154,18 +156,23 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
 
   FewLine<NT> line(a);
   uint32_t u0 = 0, u1 = 1;
+  int head_in = 0;      // of its set
   if (a.log_groups >= 0) {
+    // the workgroups of one XCD, which come in turns of eight, are neighbours
+    p = (p & 7) << (a.log_groups - 3) | p >> 3;
+    head_in = p & ((1 << a.log_heads) - 1);
     line.count();
-    const int log_groups = line.groups();
-    if (p >> log_groups) return;
-    u0 = line.cut(p, log_groups); u1 = line.cut(p + 1, log_groups);
+    const int log_groups = line.groups(), run = p >> a.log_heads;
+    if (run >> log_groups) return;
+    u0 = line.cut(run, log_groups); u1 = line.cut(run + 1, log_groups);
   }
   const uint16_t *kbase = static_cast<const uint16_t*>(a.k), *vbase = static_cast<const uint16_t*>(a.v);
   const int in_block = (1 << a.cache.shift) - 1;
 
   for (uint32_t cur = u0; cur < u1;) {
-    const auto tile = a.log_groups < 0 ? line.whole(p) : line.find(cur);
+    auto tile = a.log_groups < 0 ? line.whole(p) : line.find(cur);
     if (!tile.there) break;
+    tile.head = tile.head << a.log_heads | head_in;
     const int n = min(tile.n_units - tile.unit, (int)(u1 - cur));
     const PagedRequest r = tile.r;
     const int rows = r.fresh * a.share;
@@ -423,21 +430,23 @@ template <int N, int M, int D, class Part> __device__ __forceinline__ void few_a
   for (int i = 0; i < N; ++i) few_add(s, m[i], l[i], o[i]);
 }
 
-// Tiles that several workgroups did, their parts added in the order of the keys: there is a workgroup here for every cut p of the line, and
+// Tiles that several workgroups did, their parts added in the order of the keys: there is a workgroup here for every cut p of the line and head of a set, and
 // those whose cuts lie in one tile share its rows, 256 values to a run.  A wavefront has a run, or takes turns with others at its parts where the
 // runs are fewer (one token behind 131072 keys, 32 parts to a tile: 96.7 us with the first kernel, 99.2 where the workgroup
 // of the first cut does all runs).
 template <int D, int NT> struct FewJoin { static constexpr int kRuns = 16 * NT * D / 256, kWaves = kRuns > 8 ? kRuns : 16 / kRuns * kRuns, kThreads = 64 * kWaves; };
-template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_join(const PagedArgs& a, FewLine<NT>& line, int log_groups, int p) {
+template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_join(const PagedArgs& a, FewLine<NT>& line, int log_groups, int b) {
   constexpr int M = 16 * NT, R = FewJoin<D, NT>::kRuns, W = FewJoin<D, NT>::kWaves;
   constexpr int64_t kFloats = FewPart<D, NT>::kFloats;
   __shared__ FewSum sums[W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int p = (b >> a.log_heads) + 1, head_in = b & ((1 << a.log_heads) - 1);
   const uint32_t at = line.cut(p, log_groups);
   if (p >> log_groups || at >= line.total) return;
-  const auto tile = line.find(at);
+  auto tile = line.find(at);
   const uint32_t first = tile.first, end = first + tile.n_units;
   if (!tile.there || at == first) return;      // no part before the cut
+  tile.head = tile.head << a.log_heads | head_in;
   // the first cut behind the tile's first unit, the last one before its end: p * total / groups > first, < end
   // (mostly this one is both, which costs no division)
   auto cut_behind = [&](uint32_t unit) { return (((uint64_t)unit << log_groups) + line.total - 1) / line.total; };
@@ -452,7 +461,7 @@ template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_j
   const int e = run * 256 + lane * 4, row = e / D;
   const int n = last - p0 + 2;
   const bool whole = line.cut(p0 - 1, log_groups) == first;      // the first part is the first of its workgroup
-  auto part = [&](int k) { return a.partial + (2 * (p0 - 1 + k) + (k == 0 && !whole ? 1 : 0)) * kFloats; };
+  auto part = [&](int k) { return a.partial + (2 * ((p0 - 1 + k) << a.log_heads | head_in) + (k == 0 && !whole ? 1 : 0)) * kFloats; };
   FewSum s{-INFINITY, 0.f, f32x4{0.f, 0.f, 0.f, 0.f}};
   if (working) {
     int k = turn;
@@ -481,7 +490,7 @@ template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_j
 template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT>::kThreads)) void paged_few_join_kernel(const PagedArgs a) {
   FewLine<NT> line(a);
   line.count();
-  paged_few_join<T, D, NT>(a, line, line.groups(), blockIdx.x + 1);
+  paged_few_join<T, D, NT>(a, line, line.groups(), blockIdx.x);
 }
 
 template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs& a, hipStream_t s) {
@@ -491,7 +500,7 @@ template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs
   else hipLaunchKernelGGL((paged_few_kernel<T, D, NT, 8>), dim3(a.few_grid), dim3(512), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.log_groups < 0) return e;
-  hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3(a.few_grid - 1), dim3(FewJoin<D, NT>::kThreads), 0, s, a);
+  hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3(a.few_grid - (1 << a.log_heads)), dim3(FewJoin<D, NT>::kThreads), 0, s, a);
   return hipGetLastError();
 }
 

@@ -512,8 +512,8 @@ template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT
   line.count();
   if (line.total == 0) return;
   const int log_groups = line.groups();
-  for (int p = blockIdx.x + 1; p < a.few_grid; p += 256) {
-    paged_few_join<T, D, NT>(a, line, log_groups, p);
+  for (int b = blockIdx.x; b < a.few_grid - (1 << a.log_heads); b += 256) {
+    paged_few_join<T, D, NT>(a, line, log_groups, b);
     __syncthreads();
   }
 }
