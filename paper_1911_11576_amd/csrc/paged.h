@@ -31,6 +31,8 @@ struct PagedAttnSpec {
   int share = 1;                   // query heads to a key head
   // requests of up to few_rows rows: tiles of 16 * row_tiles, units of unit_keys keys, 1 << log_groups workgroups
   int few_rows = 0, row_tiles = 1, unit_keys = 256, log_groups = 0, few_grid = 0;
+  int log_heads = 0;               // key heads of a set, 1 << log_heads
+  bool neighbours = false;         // workgroups of an XCD have neighbouring runs
   // the others: places for tiles of 128 rows (0: there are none)
   int64_t slots = 0, few_bytes = 0, partial_bytes = 0;
 };

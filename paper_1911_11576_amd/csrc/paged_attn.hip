@@ -37,6 +37,14 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
       if (s->unit_keys >= (1 << 29)) { *err = "too many rows"; return false; }
       s->unit_keys *= 2;
     }
+    // Sets of key heads.  Where a head's rows of a block follow one another: as large a power of two as divides the heads, up to the CUs of an XCD (64
+    // requests of up to 24000 keys, 32 / 8 heads of 128: 345 us, 355 with sets of two, 361 without sets and neighbours).
+    // Where heads lie side by side and share lines of 128 bytes: two (64 of 16000, 16 / 8 heads of 32: 209 us, 226 with eight, 323 without; 24 / 4 of
+    // 96, 8000: 143 and 160).  Where they lie side by side in whole lines: none (256 of 4000, 32 / 8 of 128: 628 us, 676 with eight; 32 of 8000, 16 / 16 of 64: 170
+    // and 195; one of 131072 alone gains, 97 -> 94).
+    const int most = s->cache.slot < s->cache.head ? 5 : s->cache.head % 64 ? 1 : 0;
+    s->log_heads = std::min(most, __builtin_ctz((unsigned)d.kv_heads));
+    s->neighbours = most > 0;
     if (any) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
   }
   s->partial_bytes = s->few_bytes;
@@ -77,7 +85,7 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.unit_keys = s.unit_keys; a.log_groups = s.log_groups; a.few_grid = s.few_grid;
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.few_rows = s.few_rows;
-  a.log_heads = s.log_groups < 0 ? 0 : std::min(5, __builtin_ctz((unsigned)s.d.kv_heads));
+  a.log_heads = s.log_heads; a.neighbours = s.neighbours;
   a.head_sets = s.d.kv_heads >> a.log_heads;
   if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;
   a.slots = (int)s.slots;

@@ -23,6 +23,7 @@ struct PagedArgs {
   int unit_keys;                   // few rows: keys of a unit of work, a multiple of 32 to a wavefront
   int log_groups, few_grid;        // few rows: workgroups, 1 << log_groups of them; log_groups -1: a unit each, which is a whole tile
   int log_heads, head_sets;        // few rows: log2 of the key heads of a set, and the sets
+  int neighbours;                  // few rows: workgroups of an XCD have neighbouring runs
   int few_rows;                    // requests of up to so many rows are the few-rows kernel's, the others the tile kernel's
   float* tile_partial;             // tiles of 128 rows: up to 2 * kTileShares of [128 * (D + 2)]
   int slots;                       // places for tiles in the order of the rows

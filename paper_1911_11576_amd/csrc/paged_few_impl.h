@@ -1,15 +1,14 @@
 // Attention over a paged cache, few rows a request (single tokens, a few guessed ones): bound by the reading of keys and values.
 //
 // The work of all requests is one line of units, (request, set of key heads, tile of 16 * NT rows, run of keys), cut into equal
-// runs, one to as many workgroups as a set has heads: each finds its own from the lengths on the device, whatever their spread.  A set is the largest power of two, up to the
-// 32 CUs of an XCD, that divides the key heads: its workgroups walk the same keys of the heads at the same time behind one L2, which thereby fetches the lines that
-// heads share once (VV).  A workgroup's
+// runs, one to as many workgroups as a set has heads: each finds its own from the lengths on the device, whatever their spread.  The workgroups of a set walk the
+// same keys of its heads at the same time behind one L2, which fetches lines that heads share once.  A workgroup's
 // wavefronts take 32 keys each of a step; a wavefront brings keys and values into LDS of its own by direct loads of whole rows (no
 // barrier in the loop), the next 32 keys as soon as the first dot is through with these, their values behind the second.  At the end of a tile's run the
 // wavefronts' maxima, sums and results meet in LDS; a tile that one workgroup does from end to end is stored, parts of others go to
 // the partial results, which paged_few_join_kernel adds in the order of the keys.  Where no request can be long a workgroup has
-// one tile and all of its keys, and nothing is left to join.  6.2 TB/s for 64 requests of one token behind up to 24000 keys (32 / 8 heads of 128, 360 us; a copy of
-// 1 GiB reaches 6.6), 5.5 for one behind 131072 (97 us); keys and values through the caches 397 and 108.
+// one tile and all of its keys, and nothing is left to join.  6.5 TB/s for 64 requests of one token behind up to 24000 keys (32 / 8 heads of 128, 345 us; a copy of
+// 1 GiB reaches 6.6), 5.5 for one behind 131072 (97 us); keys and values through the caches 397 and 108 (before the sets).
 #pragma once
 #include "paged_attn_impl.h"
 
@@ -158,8 +157,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
   uint32_t u0 = 0, u1 = 1;
   int head_in = 0;      // of its set
   if (a.log_groups >= 0) {
-    // the workgroups of one XCD, which come in turns of eight, are neighbours
-    p = (p & 7) << (a.log_groups - 3) | p >> 3;
+    if (a.neighbours) p = (p & 7) << (a.log_groups - 3) | p >> 3;      // (an XCD has every eighth workgroup)
     head_in = p & ((1 << a.log_heads) - 1);
     line.count();
     const int log_groups = line.groups(), run = p >> a.log_heads;
