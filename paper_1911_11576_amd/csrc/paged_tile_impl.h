@@ -3,8 +3,8 @@
 // A workgroup has 128 rows of one request and key head, 32 to a wavefront, and walks the keys that they see 64 at a time: keys
 // and values by direct loads into LDS, the next 64 in flight to the other half while these are worked on, one
 // barrier a step.  Both dots are v_mfma_f32_32x32x16.  A tile of more than an even share of the work is split over workgroups
-// by its keys, and paged_mixed_join_kernel adds the parts in their order.  905 TFLOP/s at D 128 (8 chunks of 1 to 1024 tokens behind up to 12000 keys, 32 / 8
-// heads, 367 us; the card's rate of a bf16 product of 8192^3 is 1205), 585 at D 64 (4 prompts of 2048 x 16 heads, 58.8 us).
+// by its keys, and paged_mixed_join_kernel adds the parts in their order.  925 TFLOP/s at D 128 (8 chunks of 1 to 1024 tokens behind up to 12000 keys, 32 / 8
+// heads, 359 us; the card's rate of a bf16 product of 8192^3 is 1205), 600 at D 64 (4 prompts of 2048 x 16 heads, 57.3 us).
 #pragma once
 #include <algorithm>
 
