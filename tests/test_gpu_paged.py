@@ -465,6 +465,17 @@ def test_attention_of_thousands_of_requests(table_keys, long):
     check_attention(c, max_new=1)
 
 
+@pytest.mark.parametrize("order", ["head", "token"])
+@pytest.mark.parametrize("kv_heads, dim", [(1, 64), (2, 32), (6, 96), (12, 128), (32, 32), (48, 64), (64, 32), (100, 32), (7, 96)])
+def test_attention_of_sets_of_key_heads(kv_heads, dim, order):
+    """Heads whose workgroups walk the same keys: no set, one, several; less work than workgroups; single tokens alone and beside a chunk."""
+    rng = np.random.default_rng(kv_heads + dim)
+    for keys, new, share in (([1500, 3, 700, 64], [1, 1, 1, 1], 2), ([2, 0], [1, 0], 3), ([1300, 90, 5], [1, 70, 0], 1)):
+        c = problem(rng, "bf16", keys, new, share * kv_heads, kv_heads, dim, 16, order=order)
+        c["tables"] = np.pad(c["tables"], ((0, 0), (0, 100)), constant_values=-1)      # more than 1024 keys to a row
+        check_attention(c, max_new=max(new))
+
+
 @pytest.mark.parametrize("new", [1, 3, 90])
 def test_attention_behind_a_billion_keys(new):
     """2^30 - 5 keys, the most that a row of the table may name but five, of which a window leaves the last ones: as of a request of the same end alone."""
