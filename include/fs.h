@@ -477,7 +477,8 @@ fs_status fs_rotary_frequencies(int32_t rotary_dim, double base, double factor, 
  * lengths[b] keys, the last of them its new tokens, whose queries are rows starts[b] .. starts[b+1]-1 of q.  Query heads
  * share key heads in runs of q_heads / kv_heads.  For the query at position p, over the keys j that it sees
  *     s_j = scale * q . k_j      out = sum_j softmax(s)_j v_j      lse = log sum_j exp(s_j)
- * causal: j <= p; with a window also j > p - window.  A row that sees no key gets zeros, and -inf as log-sum-exp.
+ * causal: j <= p; with a window also j > p - window.  A row that sees no key, or none whose score is above -inf, gets zeros, and -inf as
+ * log-sum-exp.
  *   inputs    q [tokens, q_heads, head_dim], k_cache, v_cache, tables i32 [requests, table_blocks], lengths i32 [requests],
  *             starts i32 [requests+1]
  *   outputs   out [tokens, q_heads, head_dim]; with log_sum_exp also lse f32 [tokens, q_heads]
@@ -487,7 +488,7 @@ fs_status fs_rotary_frequencies(int32_t rotary_dim, double base, double factor, 
  * Rows outside every request are left as they were.  A length beyond the table's row counts as that row's, one below 0 as 0;
  * starts are cut to [0, tokens]; they do not decrease (where they do, the rows concerned are undefined).  Keys in blocks outside [0, blocks) are not
  * seen.  What lies in the cache behind a request's length is never used, whatever it is, and an infinity or NaN in a value
- * reaches only the rows that see it.
+ * reaches only the rows that see it; there an infinity stays one, or is NaN where its weight beside the largest rounds to 0 in the storage type.
  * max_new: the most new tokens that a request has, for the choice of kernels (0: unknown); a request may have more.
  * FS_F16 or FS_BF16 (the probabilities are rounded to it for the second product, all sums are fp32), head_dim 32, 64, 96 or
  * 128, strides and head strides multiples of 8, up to 65536 requests, 2^30 keys in a row of the table.  Results do not depend on timing: no atomics, a fixed order of sums.

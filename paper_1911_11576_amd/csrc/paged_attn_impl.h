@@ -94,6 +94,10 @@ __device__ __forceinline__ int wave_upto(int v) {
   return v;
 }
 
+// 2^x as the factor of what was summed up under a smaller maximum: no less than the least fp32 number, so that an infinity among it, a value's that the
+// row sees, stays one where the power is none (0 times it would be NaN; of a number nothing is left either way).
+__device__ __forceinline__ float sum_factor(float x) { return fmaxf(__builtin_amdgcn_exp2f(x), 0x1p-149f); }
+
 // Values of a 16-byte piece that are infinite or NaN: the exponent's bits are all ones, which the addition carries into the sign's place.
 template <typename T> struct Odd;
 template <> struct Odd<f16_t> { static constexpr uint32_t kMask = 0x7c007c00u, kCarry = 0x04000400u; };

@@ -266,7 +266,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
           }
         top = rows_allreduce<MaxOp>(top);
         const float low = top == -INFINITY ? 0.f : top;
-        const float keep = __builtin_amdgcn_exp2f(m[nt] - low);
+        const float keep = sum_factor(m[nt] - low);
         m[nt] = top;
         float sum = 0.f;
 #pragma unroll
@@ -354,7 +354,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
       float top = -INFINITY;
 #pragma unroll
       for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
-      const float f = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m[nt] - top);
+      const float f = top == -INFINITY ? 0.f : sum_factor(m[nt] - top);
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) {
         f32x4 x = o[nt][dt];
@@ -409,7 +409,7 @@ template <typename T, int D, int NT, int W> __global__ __launch_bounds__(64 * W,
 struct FewSum { float m, l; f32x4 o; };
 __device__ __forceinline__ void few_add(FewSum& s, float m, float l, f32x4 o) {
   const float top = fmaxf(s.m, m), low = top == -INFINITY ? 0.f : top;
-  const float f = __builtin_amdgcn_exp2f(s.m - low), h = __builtin_amdgcn_exp2f(m - low);
+  const float f = sum_factor(s.m - low), h = sum_factor(m - low);
 #pragma unroll
   for (int j = 0; j < 4; ++j) s.o[j] = s.o[j] * f + o[j] * h;
   s.l = s.l * f + l * h;

@@ -379,7 +379,7 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile(const Pa
     // the sums are rescaled where a maximum has grown by more than 2^8: below that the exponentials are as exact
     if (__ballot(top > m && !((top - m) * scale2 <= 8.f))) {
       const float grown = fmaxf(m, top);
-      const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - grown) * scale2);
+      const float keep = m == -INFINITY ? 1.f : sum_factor((m - grown) * scale2);      // (of nothing but an infinity or NaN that was added: as it is)
       m = grown;
       l *= keep;
 #pragma unroll

@@ -530,6 +530,53 @@ def test_attention_values_that_some_rows_do_not_see(new, keys, value):
         check_out(dict(c, q=c["q"][clean]), [outs[0][clean], outs[1][clean]], [a[clean] for a in part], f"rows before a {value}")
 
 
+def put_value(c, request, key, value, every=5):
+    """`value` in every fifth element of the value of a request's key, whose key itself stays as it is."""
+    page = int(c["tables"][request, key // c["block_size"]])
+    v = c["caches"][1] if c["order"] == "head" else c["caches"][1].transpose(1, 2)
+    v[page, :, key % c["block_size"], ::every] = value
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+@pytest.mark.parametrize("keys, new, places, window", [
+    (3, 3, [0], 0), (40, 3, [0, 38], 0), (40, 3, [20, 37], 20), (500, 1, [0, 250, 499], 0), (40000, 2, [0, 20000, 39999], 0),      # few rows: one workgroup, several
+    (150, 150, [0], 0), (150, 150, [63, 149], 0), (300, 70, [0, 230, 299], 0), (300, 150, [150, 200], 100), (9000, 60, [0, 4000, 8990], 0)])      # tiles; of split keys
+def test_attention_of_values_that_are_infinite(dtype, value, keys, new, places, window):
+    """Infinities or NaN in values alone, their keys numbers: the rows that see them have them as the definition does, the others do not."""
+    c = problem(np.random.default_rng(keys), dtype, [keys, 7], [new, 1], 4, 2, 64, 16)
+    for k in places:
+        put_value(c, 0, k, value)
+    with np.errstate(invalid="ignore"):
+        want = wanted(c, window)
+    plan, nbytes = plan_of(c, window)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+    check_out(c, outs, want, plan_text(c, window, value))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("keys, new", [(600, 1), (40000, 2), (150, 150), (9000, 60)])
+def test_attention_of_infinite_values_behind_a_small_weight(dtype, keys, new):
+    """Scores of the last keys are 320 above those before them: what was summed up until then is taken times e^-320, which fp32 has no number
+    for, and an infinity among it stays one, inside a run of keys, between wavefronts and between parts."""
+    c = problem(np.random.default_rng(keys), dtype, [keys], [new], 4, 2, 64, 16)
+    high = 64 if keys == 150 else keys - 64
+    c["q"] = torch.ones_like(c["q"])
+    for k in range(high, keys):
+        c["caches"][0][c["tables"][0, k // 16], :, k % 16] = 40.0
+    put_value(c, 0, 0, float("inf"))
+    with np.errstate(invalid="ignore"):
+        want = wanted(c)
+    assert np.isposinf(want[0]).any()
+    plan, nbytes = plan_of(c)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+    check_out(c, outs, want, plan_text(c))
+
+
 def test_attention_scores_of_any_size():
     c = problem(np.random.default_rng(9), "bf16", [500, 90], [1, 60], 4, 2, 64, 16, spread=8.0)
     check_attention(c)
