@@ -39,7 +39,7 @@ struct TileWork {
 // The order of the work, made by every wavefront for itself from the lengths on the device, up to 64 requests of many rows one to a lane.  A tile's
 // time goes with its steps, which differ up to the whole length of the longest request, and workgroups start in order as others end.
 // So: the tiles of more steps than an even share of all work, that of few rows with it (63 requests of one token behind 2000 keys and one
-// of 1000: 125 us, 155 where shares are of the tiles alone), are split into parts of at most that and come first; the
+// of 1000: 119 us, 155 where shares are of the tiles alone; 400 behind 200 and four of 256 behind 1744: 147, 162 where steps of short requests get lost), are split into parts of at most that and come first; the
 // others follow by falling steps.  Steps do not fall along a request's tiles, so how many of them have at least s is a
 // formula, and the k-th tile is found by bisection over s.  (Chunks of 1 to 1024 tokens behind contexts of up to 12000: the longest tile alone is 1.2
 // times the even share; request by request the launch took 1.48 times it.)  A share is 1.25 times a 512th, so that parts of one length do
@@ -52,7 +52,7 @@ struct TileLine {
   int share_steps = 0;           // an even share
   int split = 0, parts = 1;      // the lane's tiles of more steps than that (its last ones), and the parts of each
   int items = 0;                 // parts of all
-  int others = 0;                // steps of requests of few rows that the lane looked at, in 64s
+  int64_t others = 0;            // steps of requests of few rows that the lane looked at, over all key heads
 
   __device__ __forceinline__ explicit TileLine(const PagedArgs& args) : a(args) {}
   __device__ __forceinline__ PagedRequest request(int b) const { return b < a.requests ? paged_request(a, b) : PagedRequest{}; }
@@ -84,7 +84,7 @@ struct TileLine {
   // 64 keys of a tile of few rows, which memory bounds, take a place on a CU as long as a step of 128 rows
   __device__ __forceinline__ void look(const PagedRequest& r) {
     const int rows = r.fresh * a.share;
-    if (rows > 0 && rows <= a.few_rows) others = (int)min((int64_t)others + ((int64_t)((r.keys - paged_first_key(a, r) + 63) >> 6) * a.kv_heads >> 6), (int64_t)1 << 24);
+    if (rows > 0 && rows <= a.few_rows) others += (int64_t)((r.keys - paged_first_key(a, r) + 63) >> 6) * a.kv_heads;
   }
   __device__ __forceinline__ void measure() {
     const int rows = mine.fresh * a.share;
@@ -113,8 +113,10 @@ struct TileLine {
     }
     measure();
     const int last = last_steps(), first = flat >= 0 || tiles == 0 ? last : max(0, mine.keys - mine.fresh + 64) >> 6;
-    // (in 64 steps: no more than 2^31 of them)
-    const int total = wave_sum((int)min(others + ((int64_t)tiles * (first + last) * a.kv_heads >> 7), (int64_t)1 << 24));
+    // in 64 steps, no more than 2^31 of them; what the lanes have beside whole 64s is summed up too (500 requests of seven steps and eight heads
+    // are 28000 steps, none of which is 64 of one request)
+    const int64_t halves = 2 * others + (int64_t)tiles * (first + last) * a.kv_heads;      // of steps
+    const int total = wave_sum((int)min(halves >> 7, (int64_t)1 << 24)) + (wave_sum((int)(halves & 127)) >> 7);
     share_steps = min(1 << 23, max(kLeastSteps, (total + total / 4) / (kTileShares / 64)));      // (a tile has up to 2^24)
     for (;; share_steps *= 2) {      // (never more parts than there is room for)
       split = at_least(share_steps + 1);

@@ -447,6 +447,17 @@ def test_attention_of_chunks_among_many_requests(requests, chunks):
     check_attention(c, causal=False)
 
 
+@pytest.mark.parametrize("singles, behind, split", [(0, 0, True), (500, 448, False), (30, 12, True)])
+def test_attention_counts_short_requests_in_the_shares(singles, behind, split):
+    """A chunk of 32 steps of 64 keys is split over workgroups where it is all there is, not where hundreds of requests of seven steps a head
+    make an even share longer than it.  Parts of split tiles are written to the last 2 * 512 places of the partial results."""
+    dim, heads = 32, 8
+    c = problem(np.random.default_rng(singles), "f16", [behind] * (singles // 2) + [2048] + [behind] * (singles - singles // 2), [1] * (singles // 2) + [128] + [1] * (singles - singles // 2),
+                heads, heads, dim, 16)
+    outs = check_attention(c)
+    assert bool((outs[-1][-2 * 512 * 128 * (dim + 2) * 4:] != 255).any()) == split
+
+
 @pytest.mark.parametrize("table_keys, long", [(64, 60), (2048, 1900)])
 def test_attention_of_thousands_of_requests(table_keys, long):
     """More than 4096 requests, single tokens: a workgroup each tile, and equal runs whose ends are searched behind the first 4096."""
