@@ -202,7 +202,7 @@ fs_status fs_plan_create_rotary(const fs_rotary_desc* desc, fs_plan** out) {
     }
     g.bytes = 2 * t * dim * s.heads * e + t * (store ? 8 : 4) + 4ll * d.rotary_dim;
     p->description = numbers("rotary[GRID-WARP,THREAD] width=%lld, units=%lld, heads_each=%lld; cta_num=%lld, cta_size=256", s.width, s.units, s.heads_each,
-                             (t * s.units * s.groups + 255) / 256) + (store ? ", stores k and v in the cache" : "");
+                             (t * s.units * s.groups + 255) / 256) + (store ? ", stores k and v in the cache" : s.once ? ", stores past the caches" : "");
     return true;
   });
 }

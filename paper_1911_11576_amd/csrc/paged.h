@@ -21,7 +21,7 @@ struct RotarySpec {
   int width = 1;                   // elements of a vector
   int units = 1, heads = 1;        // threads to a head, heads in all (of q, k and stored v)
   int heads_each = 1, groups = 1;  // heads of a thread, threads that share the heads
-  bool once = false;               // stores past the caches
+  bool once = false;               // stores past the caches, where the outputs begin at lines of 128 bytes
   bool one = false;                // a vector of a head to a thread
   int most_angles = 0;             // several heads to a thread: angles of a workgroup's rows
 };

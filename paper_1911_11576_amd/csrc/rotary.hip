@@ -36,6 +36,7 @@ struct RotaryArgs {
   Divisor by_lanes, by_units, by_pairs;
   int most_angles;                   // of a workgroup's rows
   float magnitude;
+  bool once;                         // of the launch: stores past the caches
 };
 
 // W elements at element alignment times W: one access of up to 16 bytes.
@@ -216,7 +217,7 @@ template <typename T, int W, int H, int LAYOUT, bool STORE, bool ONCE> __global_
 template <typename T, int W, int H, int LAYOUT> void launch_heads(const RotaryArgs& a, const RotarySpec& s, unsigned wgs, hipStream_t stream) {
   const size_t lds = H > 1 && W == 8 ? 8 * (size_t)s.most_angles : 0;
   if (s.d.blocks > 0) hipLaunchKernelGGL((rotary_kernel<T, W, H, LAYOUT, true, false>), dim3(wgs), dim3(256), lds, stream, a);
-  else if (s.once) hipLaunchKernelGGL((rotary_kernel<T, W, H, LAYOUT, false, true>), dim3(wgs), dim3(256), lds, stream, a);
+  else if (a.once) hipLaunchKernelGGL((rotary_kernel<T, W, H, LAYOUT, false, true>), dim3(wgs), dim3(256), lds, stream, a);
   else hipLaunchKernelGGL((rotary_kernel<T, W, H, LAYOUT, false, false>), dim3(wgs), dim3(256), lds, stream, a);
 }
 template <typename T, int W, int LAYOUT> void launch_layout(const RotaryArgs& a, const RotarySpec& s, unsigned wgs, hipStream_t stream) {
@@ -261,7 +262,10 @@ template <typename T> hipError_t launch_type(const RotaryArgs& a, const RotarySp
 // Where a half of a head is no whole line of 128 bytes, or a part of it is not turned, a thread has one vector of a head: 8191 rows of those 72 heads of
 // 64 in fp16, half of each turned, into a cache 26.9 us (5.6 TB/s), with two vectors 30.5; all of each turned 27.9 and 30.6.  Where halves are lines two are
 // better: 55.4 and 57.8 for the first of these.  Stores go past the caches where two vectors fill whole lines each and are not for a cache, which attention reads next: 66.8 ->
-// 60.0 us for the first (before the rest); with one vector 12286 rows of 48 heads of 64 25.8 -> 27.3, where lines are not filled 33 -> 41.
+// 60.0 us for the first (before the rest); with one vector 12286 rows of 48 heads of 64 25.8 -> 27.3, where lines are not filled 33 -> 41.  So not where the
+// outputs' rows or buffers begin inside lines: the first with rows 16 bytes longer 67.0 us through the caches and 80.3 past them, its buffers 16 bytes behind a
+// line 64.8 and 88.4, 64 bytes 61.0 and 63.2; the fp32 case 22.6 and 39.8, 22.7 and 38.2, 22.5 and 27.9.  Rows 64 bytes longer, of which every
+// other one begins at a line: 68.4 and 58.7, in fp32 22.7 and 25.1.  Vectors of less than 16 bytes: 77.0 and 76.8, in fp32 26.5 and 27.2.
 void rotary_geometry(RotarySpec* s) {
   const fs_rotary_desc& d = s->d;
   const int64_t threads = (int64_t)d.tokens * s->units * s->heads, bytes = (d.dtype == FS_F32 ? 4 : 2) * (int64_t)d.head_dim;
@@ -273,7 +277,8 @@ void rotary_geometry(RotarySpec* s) {
     s->units = pieces;
     s->heads_each = 4;
   }
-  s->once = lines;
+  const int64_t whole = 32;      // 128 bytes of fp32, 64 of the others
+  s->once = lines && d.blocks == 0 && s->width == (d.dtype == FS_F32 ? 4 : 8) && d.q_out_stride % whole == 0 && (d.k_heads == 0 || d.k_out_stride % whole == 0);
   s->groups = (s->heads + s->heads_each - 1) / s->heads_each;
   s->most_angles = (254 / (s->units * s->groups) + 2) * (d.rotary_dim / 2);      // 256 threads are of no more rows
 }
@@ -299,6 +304,7 @@ int rotary_launch(const RotarySpec& s, const void* const* in, void* const* out, 
   a.units = s.units; a.groups = s.groups; a.by_units = divisor(s.units); a.by_lanes = divisor(s.units * s.groups); a.by_pairs = divisor(s.d.rotary_dim / 2);
   a.most_angles = s.most_angles; a.inverse = s.d.inverse;
   a.magnitude = (float)s.d.magnitude;
+  a.once = s.once && ((reinterpret_cast<uintptr_t>(a.q_out) | reinterpret_cast<uintptr_t>(a.k_out)) & 127) == 0;
   hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = s.d.dtype == FS_F32 ? launch_type<float>(a, s, st) : s.d.dtype == FS_F16 ? launch_type<f16_t>(a, s, st) : launch_type<bf16_t>(a, s, st);
   if (e != hipSuccess) { *err = std::string("rotary launch: ") + hipGetErrorString(e); return -1; }

@@ -146,6 +146,15 @@ def test_plans_report():
         assert plan.info()["schedule"] == "paged_attention" and plan.info()["algorithmic_bytes"] > 0 and "paged_attention" in plan.describe()
 
 
+@pytest.mark.parametrize("change, once", [
+    (dict(), True), (dict(dtype="f32", head_dim=64), True), (dict(q_out_stride=32 * 128 + 64), True), (dict(q_out_stride=32 * 128 + 32, k_out_stride=8 * 128 + 32), True),
+    (dict(q_out_stride=32 * 128 + 8), False), (dict(k_out_stride=8 * 128 + 8), False), (dict(dtype="f32", q_out_stride=32 * 128 + 16), False), (dict(q_stride=32 * 128 + 2), False),
+    (dict(q_out_stride=32 * 128 + 2), False), (dict(rotary_dim=64), False), (dict(head_dim=64), False), (dict(k_heads=0), True), (dict(blocks=600, block_size=16), False)])
+def test_rotary_stores_past_the_caches_in_whole_lines_alone(change, once):
+    with Plan.rotary(**dict(dict(dtype="bf16", tokens=8192, q_heads=32, k_heads=8, head_dim=128), **change)) as p:
+        assert ("past the caches" in p.describe()) == once, p.describe()
+
+
 @pytest.mark.parametrize("dim", [2, 24, 128])
 @pytest.mark.parametrize("args", [{}, dict(base=5e5), dict(factor=4.0), dict(factor=8.0, low=1.0, high=4.0, original=8192.0), dict(factor=2.0, low=1.0, high=32.0, original=100.0)])
 def test_frequencies(dim, args):
