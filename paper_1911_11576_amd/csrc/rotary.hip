@@ -224,7 +224,9 @@ template <typename T, int W, int LAYOUT> void launch_layout(const RotaryArgs& a,
   if constexpr (W == 8 && LAYOUT == kHalves)
     if (s.one) return launch_heads<T, W, 4, kOneVector>(a, s, wgs, stream);
   if (s.heads_each == 1) launch_heads<T, W, 1, LAYOUT>(a, s, wgs, stream);
-  else launch_heads<T, W, (W == 8 ? 2 : 8), LAYOUT>(a, s, wgs, stream);
+  else if constexpr (W == 8) launch_heads<T, W, 2, LAYOUT>(a, s, wgs, stream);
+  else if (s.heads_each == 4) launch_heads<T, W, 4, LAYOUT>(a, s, wgs, stream);
+  else if constexpr (W * sizeof(T) != 8) launch_heads<T, W, 8, LAYOUT>(a, s, wgs, stream);
 }
 
 template <typename T, int W> hipError_t launch_width(RotaryArgs a, const RotarySpec& s, hipStream_t stream) {
@@ -258,7 +260,11 @@ template <typename T> hipError_t launch_type(const RotaryArgs& a, const RotarySp
 // Several heads to a thread are requested together and share its angles, where that leaves the chip two wavefronts a SIMD (32 rows of 48
 // heads 4.0 us, with several 4.9).  16-bit vectors: two of them, angles made by the workgroup: 16384 rows of 40 heads of 128 in bf16 55.4 us (6.05 TB/s;
 // 59.6 with four and angles of the thread's own, 79 with one; 55.7 with four), 24 + 24 + 24 heads of 64 into a cache 30.5.  fp32, whose vectors have half the angles:
-// eight, angles of its own: 8192 rows of 32 heads of 64 21.6 us (22.2 with the workgroup's; 24.3 with four, 25.8 with one).
+// eight, angles of its own: 8192 rows of 32 heads of 64 21.6 us (22.2 with the workgroup's; 24.3 with four, 25.8 with one).  Where there are fewer than 16
+// heads four, fewer than four one: a thread reads as many whatever there are (fp32, heads of 80 with 24 turned: 16384 rows of 8 heads 18.7 us, with eight 21.3;
+// 65536 of two 21.3, with four 23.5, with eight 34.6).  Vectors of 8 bytes: four (bf16, 8192 rows of 40 heads of 128, strides of 4 more 32.1 us, with eight 34 to 37.6, with
+// two 38.9, with one 43.8; of 80, 40 turned 25.9, 27.1, 27.1, 31.8: 4.05 TB/s); of 4 and 2 bytes eight as well (strides of 2 more 31.3, with four 32.6, with one 51.5).
+// Interleaved, in vectors of 16 bytes: the gradient's sizes 56.0 us.
 // Where a half of a head is no whole line of 128 bytes, or a part of it is not turned, a thread has one vector of a head: 8191 rows of those 72 heads of
 // 64 in fp16, half of each turned, into a cache 26.9 us (5.6 TB/s), with two vectors 30.5; all of each turned 27.9 and 30.6.  Where halves are lines two are
 // better: 55.4 and 57.8 for the first of these.  Stores go past the caches where two vectors fill whole lines each and are not for a cache, which attention reads next: 66.8 ->
@@ -270,7 +276,7 @@ void rotary_geometry(RotarySpec* s) {
   const fs_rotary_desc& d = s->d;
   const int64_t threads = (int64_t)d.tokens * s->units * s->heads, bytes = (d.dtype == FS_F32 ? 4 : 2) * (int64_t)d.head_dim;
   const bool lines = bytes % 256 == 0 && (d.interleaved || d.rotary_dim == d.head_dim);
-  s->heads_each = threads < 4 * 131072 ? 1 : s->width == 8 ? 2 : 8;
+  s->heads_each = threads < 4 * 131072 ? 1 : s->width == 8 ? 2 : s->heads < 4 ? 1 : s->heads < 16 || s->width * (d.dtype == FS_F32 ? 4 : 2) == 8 ? 4 : 8;
   const int pieces = d.head_dim / 8;
   s->one = s->heads_each == 2 && !d.interleaved && !lines && (pieces & (pieces - 1)) == 0;
   if (s->one) {

@@ -231,6 +231,49 @@ def test_rotary_of_many_rows(dtype, heads, dim, rot, interleaved, store):
         assert torch.equal(same[~keep], q_out[~keep]) and torch.equal(same[keep], x[0][keep])
 
 
+@pytest.mark.parametrize("dtype, q_heads, k_heads, dim, rot, interleaved, store, pad, each", [
+    ("bf16", 11, 9, 80, 40, False, False, 0, 4), ("f16", 32, 8, 128, 24, False, True, 0, 4), ("f16", 7, 7, 20, 12, True, False, 4, 4), ("bf16", 13, 4, 36, 20, False, False, 2, 8),
+    ("f16", 9, 9, 22, 22, False, True, 0, 8), ("bf16", 16, 1, 24, 24, False, False, 3, 8), ("f16", 5, 1, 24, 10, True, False, 6, 4), ("f32", 12, 4, 36, 20, False, False, 2, 4), ("f32", 15, 1, 10, 10, False, False, 1, 8),
+    ("f32", 5, 2, 64, 64, False, True, 0, 4), ("f32", 2, 1, 64, 64, True, False, 0, 1), ("f32", 9, 1, 80, 24, False, False, 4, 4), ("bf16", 2, 1, 80, 40, False, False, 0, 1)])
+def test_rotary_of_many_rows_in_narrow_vectors(dtype, q_heads, k_heads, dim, rot, interleaved, store, pad, each):
+    """Rotated parts and strides that leave vectors of less than 16 bytes, or few heads: as many heads to a thread as their rule says, rows of outputs
+    further apart than their heads."""
+    rng, g = np.random.default_rng(dim + rot), torch.Generator("cuda").manual_seed(dim)
+    tokens = 4 * 131072 // (q_heads + k_heads) // max(1, dim // 16) + 3
+    heads = [q_heads, k_heads] + [k_heads] * store
+    wide = [torch.randn((tokens, h * dim + pad), device="cuda", generator=g).to(DT[dtype]) for h in heads]
+    x = [f64(w[:, :h * dim]).reshape(tokens, h, dim) for w, h in zip(wide, heads)]
+    freqs, pos = fs_rotary_frequencies(rot), positions_of(rng, tokens, 1 << 17)
+    frq, p = torch.tensor(freqs, dtype=torch.float64, device="cuda"), i32(pos)
+    want = [paged.rotary(a, pos, freqs, interleaved, magnitude=0.75) for a in x[:2]]
+    room = [rotary_bound(a, w, freqs, interleaved, 0.75, dtype) for a, w in zip(x, want)]
+    kw = dict(interleaved=interleaved, magnitude=0.75, q_stride=q_heads * dim + pad, k_stride=k_heads * dim + pad, q_out_stride=q_heads * dim + pad)
+    out = [torch.full_like(w, 5.0) for w in wide[:2]]
+    if store:
+        blocks = -(-tokens // 32) + 1
+        slots = rng.permutation(blocks * 32)[:tokens]
+        slots[::7] = -1
+        caches = [torch.full((blocks, k_heads, 32, dim), 7.0, dtype=DT[dtype], device="cuda") for _ in range(2)]
+        kw |= dict(v_stride=k_heads * dim + pad, blocks=blocks, block_size=32)
+        ins, outs = [*wide, p, frq, i32(slots)], [out[0], *caches]
+        want[0][slots < 0], room[0][slots < 0] = 5.0, 0
+    else:
+        kw |= dict(k_out_stride=k_heads * dim + pad)
+        ins, outs = [*wide, p, frq], out
+    with Plan.rotary(dtype, tokens, q_heads, k_heads, dim, rot, **kw) as plan:
+        assert f"heads_each={each};" in plan.describe(), plan.describe()
+        plan.launch(ins, outs)
+    within(f64(out[0][:, :q_heads * dim]).reshape(tokens, q_heads, dim), want[0], room[0], "q")
+    assert (out[0][:, q_heads * dim:] == 5).all()
+    if store:
+        empty = np.full((blocks, k_heads, 32, dim), 7.0)
+        within(f64(caches[0]), paged.stored(empty, want[1], slots), paged.stored(0 * empty, room[1], slots), "k")
+        assert np.array_equal(f64(caches[1]), paged.stored(empty, x[2], slots))
+    else:
+        within(f64(out[1][:, :k_heads * dim]).reshape(tokens, k_heads, dim), want[1], room[1], "k")
+        assert (out[1][:, k_heads * dim:] == 5).all()
+
+
 def test_rotary_gradient():
     """Against the formula's own (the transpose) and against differences, through torch's autograd."""
     t, h, d = 6, 2, 32
