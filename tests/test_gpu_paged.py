@@ -415,6 +415,28 @@ def test_attention(dtype, dim, shape):
     check_attention(c, max_new=(0, max(new))[shape % 2])
 
 
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_attention_of_fp16_heads_of_96(shape):
+    keys, new, q_heads, kv_heads, block = SHAPES[shape]
+    c = problem(np.random.default_rng(shape), "f16", keys, new, q_heads, kv_heads, 96, block, order=("token", "head")[shape % 2], pad_rows=shape % 3)
+    check_attention(c, max_new=(max(new), 0)[shape % 2])
+    check_attention(c, window=60)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+def test_attention_of_many_query_heads_to_a_key_head(dtype, dim):
+    """17 and 32 of them: tiles of 32 rows beside tiles of 128, alone, in equal runs, and a workgroup each."""
+    rng = np.random.default_rng(dim)
+    for keys, new, share in (([300, 90, 40, 700, 5], [1, 30, 2, 1, 0], 17), ([40, 200], [5, 1], 32), ([3000, 64, 1700], [1, 1, 1], 32), ([200, 17, 1000], [1, 1, 1], 17)):
+        c = problem(rng, dtype, keys, new, 2 * share, 2, dim, 16, order=("head", "token")[share == 32], pad_rows=1)
+        check_attention(c, max_new=max(new))
+    check_attention(c, max_new=0)
+    check_attention(c, causal=False)
+    keys = [int(k) for k in rng.integers(1, 60, 140)]
+    check_attention(problem(rng, dtype, keys, [1] * 140, 34, 2, dim, 16), max_new=1)      # more tiles than CUs
+
+
 @pytest.mark.parametrize("shape", [1, 3, 4, 5, 7, 9])
 @pytest.mark.parametrize("window, causal", [(0, False), (1, True), (13, True), (64, True), (100, True), (100000, True)])
 def test_attention_masks(shape, window, causal):
@@ -629,6 +651,29 @@ def test_attention_of_infinite_values_behind_a_small_weight(dtype, keys, new):
         outs = buffers(c, nbytes)
         plan.launch(inputs(c), outs)
     check_out(c, outs, want, plan_text(c))
+
+
+@pytest.mark.parametrize("keys, new", [(40, 3), (3000, 1), (150, 150), (9000, 60)])
+def test_attention_of_scores_of_minus_infinity(keys, new):
+    """Keys whose scores are -inf have no weight; a row of nothing else is like one that sees no key."""
+    c = problem(np.random.default_rng(keys), "bf16", [keys, keys], [new, new], 4, 2, 64, 16)
+    c["q"][..., 0] = 1.0
+    low = list(range(0, keys, 3)) + list(range(keys - keys // 4, keys - 1))
+    for b, some in ((0, [k for k in low if k != 1]), (1, range(keys))):
+        for k in some:
+            c["caches"][0][c["tables"][b, k // 16], :, k % 16, 0] = float("-inf")
+    plan, nbytes = plan_of(c)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+    with np.errstate(invalid="ignore"):
+        out, lse, weight, small, top = (a[:new] for a in wanted(c))
+    seen = np.isfinite(out).all((1, 2))                               # (the first row of a prompt sees one key, whose score is -inf)
+    assert seen[1:].all()
+    top[:] = 64 * 0.125 * 36                                          # of the finite ones: |q| and |k| are below 6
+    check_out(dict(c, q=c["q"][:new][seen]), [outs[0][:new][seen], outs[1][:new][seen]], [a[seen] for a in (out, lse, weight, small, top)], plan_text(c))
+    none = np.concatenate([~seen, np.ones(new, bool)])
+    assert (f64(outs[0])[none] == 0).all() and (f64(outs[1])[none] == -np.inf).all()
 
 
 def test_attention_scores_of_any_size():
