@@ -123,12 +123,12 @@ template <typename T> __device__ __forceinline__ u32x4 without_odd(u32x4 v) {
 // all loads in flight, the next step's among them; there is no register that it writes.  The code waits by itself, below.)
 // ONCE: read by nobody else, past the caches.
 template <int I, bool ONCE> __device__ __forceinline__ void load_lds16(const uint16_t* from, uint32_t lds) {
-  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2 nt" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory", "m0");
-  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory", "m0");
+  if constexpr (ONCE) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2 nt" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory");
+  else asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off offset:%2" ::"s"(lds + 960 * I), "v"(from), "n"(64 * I) : "memory");
 }
 // 4 bytes a lane
 __device__ __forceinline__ void load_lds4(const int* from, uint32_t lds) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory", "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off" ::"s"(lds), "v"(from) : "memory");
 }
 // until all but the last N loads are there (they come in order)
 template <int N> __device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
