@@ -453,7 +453,7 @@ fs_status fs_plan_create_block_tables(const fs_block_tables_desc* desc, fs_plan*
  *   A row whose slot is outside [0, blocks * block_size) is padding: nothing is written for it, not even q.  Two rows of
  *   one call with the same slot leave the slot's contents undefined.
  * Strides run from token to token, 0: dense; q, k and v may be parts of one packed projection (interleaved: even strides).
- * FS_F32, FS_F16 or FS_BF16, head_dim and rotary_dim even, head_dim up to 512, k_heads 0 (without a cache): q alone, no k among inputs and outputs.
+ * FS_F32, FS_F16 or FS_BF16, head_dim and rotary_dim even, head_dim up to 512 (attention over the cache takes fewer of both, below), k_heads 0 (without a cache): q alone, no k among inputs and outputs.
  * Errors: FS_ERR_INVALID, FS_ERR_NOMEM. */
 typedef struct {
   int32_t dtype;                   /* of q, k, v, their outputs and the cache */
@@ -489,10 +489,13 @@ fs_status fs_rotary_frequencies(int32_t rotary_dim, double base, double factor, 
  * starts are cut to [0, tokens]; they do not decrease (where they do, the rows concerned are undefined).  Keys in blocks outside [0, blocks) are not
  * seen.  What lies in the cache behind a request's length is never used, whatever it is, and an infinity or NaN in a value
  * reaches only the rows that see it; there an infinity stays one, or is NaN where its weight beside the largest rounds to 0 in the storage type.
- * max_new: the most new tokens that a request has, for the choice of kernels (0: unknown); a request may have more.
+ * max_new: the most new tokens that a request has, for the choice of kernels (0: unknown); a request may have more.  A step of single tokens takes 4 to
+ * 42 % longer without it.
  * FS_F16 or FS_BF16 (the probabilities are rounded to it for the second product, all sums are fp32), head_dim 32, 64, 96 or
- * 128, strides and head strides multiples of 8, up to 65536 requests, 2^30 keys in a row of the table.  Results do not depend on timing: no atomics, a fixed order of sums.
- * Errors: FS_ERR_INVALID, FS_ERR_UNSUPPORTED (a head_dim or stride that no kernel takes), FS_ERR_NOMEM. */
+ * 128, strides and head strides multiples of 8, up to 65536 requests, tokens * q_heads up to 2^30, 2^30 keys in a row of the table; where a request may
+ * have more than 32 rows (max_new * q_heads / kv_heads), (tokens * q_heads / kv_heads / 128 + requests) * kv_heads up to 2^24 - 2048.  Results do not
+ * depend on timing: no atomics, a fixed order of sums.
+ * Errors: FS_ERR_INVALID, FS_ERR_UNSUPPORTED (a type, head_dim, stride or number of keys or tiles that no kernel takes), FS_ERR_NOMEM. */
 typedef struct {
   int32_t dtype;                   /* FS_F16 or FS_BF16: q, caches, out */
   int32_t requests, tokens, q_heads, kv_heads, head_dim;

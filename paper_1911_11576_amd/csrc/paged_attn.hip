@@ -12,6 +12,8 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   const int64_t rows = (int64_t)(d.max_new ? std::min(d.max_new, d.tokens) : d.tokens) * s->share;      // of a request
   // Up to 32 rows are one tile of the kernel that reads each key once.  Beyond, tiles of 128 (D 128, 32 / 8 heads, 30 requests of 4000 keys: 36
   // rows 119 us, with two of these tiles 179; 32 rows 100, as a tile of 128 120; D 64, 16 / 16: 30 rows 90 and 106, 60 rows 167 and 107).
+  // (max_new 0 counts all rows of the call as one request's: single tokens are done by the mixed launch then, 64 behind up to 24000 keys in 261 us instead of
+  // 250, 48 behind up to 900 in 25.1 instead of 20.9, 256 behind up to 500 in 62.9 instead of 44.2)
   const bool many = rows > 32;
   // rows to a tile of the few-rows kernel: 16 where that is what a request has (64 of 4000 keys 168 us, 184 in tiles of 32), else 32
   s->row_tiles = (many ? s->share : rows) <= 16 ? 1 : 2;

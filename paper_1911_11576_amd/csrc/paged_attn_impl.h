@@ -31,7 +31,8 @@ struct PagedArgs {
 
 // Workgroups of the tile kernel that the chip holds, two to a CU: what is shared out evenly.
 constexpr int kTileShares = 512;
-// A tile is not split into parts of fewer steps of 64 keys (D 128, 32 / 8 heads, 128 tokens behind 1920: 26.6 us with 4, 28.9 with 8, 37.5 with
+// An even share has no fewer steps of 64 keys; parts may have, since a request's split tiles are all cut into as many even parts as its longest
+// needs (of nine steps: four and five) (D 128, 32 / 8 heads, 128 tokens behind 1920: 26.6 us with 4, 28.9 with 8, 37.5 with
 // 16; twice 64 behind 4032: 32.9, 30.0, 37.9; 512 and 256 behind 512 and 1792: 44.6, 44.1, 42.7).
 constexpr int kLeastSteps = 8;
 // Requests among which those of many rows are looked for, two times 256 (one of 512 tokens behind 32256 keys and 100 of one behind 4095: 772 us with

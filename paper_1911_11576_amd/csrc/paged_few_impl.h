@@ -7,7 +7,7 @@
 // barrier in the loop), the next 32 keys as soon as the first dot is through with these, their values behind the second.  At the end of a tile's run the
 // wavefronts' maxima, sums and results meet in LDS; a tile that one workgroup does from end to end is stored, parts of others go to
 // the partial results, which paged_few_join_kernel adds in the order of the keys.  Where no request can be long a workgroup has
-// one tile and all of its keys, and nothing is left to join.  6.5 TB/s for 64 requests of one token behind up to 24000 keys (32 / 8 heads of 128, 345 us; a copy of
+// one tile and all of its keys, and nothing is left to join.  6.5 TB/s for 64 requests of one token behind up to 24000 keys (32 / 8 heads of 128, 346 us; a copy of
 // 1 GiB reaches 6.6), 5.5 for one behind 131072 (97 us); keys and values through the caches 397 and 108 (before the sets).
 #pragma once
 #include "paged_attn_impl.h"
@@ -68,7 +68,8 @@ template <int NT> struct FewLine {
   }
   // where workgroup p's run begins
   __device__ __forceinline__ uint32_t cut(int p, int log_groups) const { return (uint32_t)((uint64_t)p * total >> log_groups); }
-  // log2 of the workgroups that have work, of one key head of a set: at least a unit each
+  // log2 of the workgroups that have work, of one key head of a set: at least a unit each, so as many as the largest power of two among the units (32 / 8
+  // heads of 128, one token behind 31 units of 256 keys 18.6 us, which 16 workgroups of a head do, behind 32 14.7, 33 17.5, 63 19.3, 64 19.4)
   __device__ __forceinline__ int groups() const { return min(a.log_groups - a.log_heads, 31 - __clz((int)max(total, 1u))); }
   struct Tile { int b, head, row0, unit, n_units; uint32_t first; PagedRequest r; bool there; };      // first: the tile's first unit in the line
   // the p-th tile, where a unit is one; of more than 64 requests the tile at place p, which takes fewer looks at their lengths
@@ -281,6 +282,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
         for (int dt = 0; dt < DT; ++dt)
 #pragma unroll
           for (int i = 0; i < 4; ++i) o[nt][dt][i] *= keep;
+        // rounded to T for the second dot alone: half a step of each weight, where fp32 weights would take that dot twice; the sum is of them unrounded
         pb[nt] = u32x4{Mfma<T>::pack(s[nt][0][0], s[nt][0][1]), Mfma<T>::pack(s[nt][0][2], s[nt][0][3]), Mfma<T>::pack(s[nt][1][0], s[nt][1][1]), Mfma<T>::pack(s[nt][1][2], s[nt][1][3])};
       }
       if (more) wait_loads<N + 1>();      // the values are there (the next keys may not be)
@@ -434,7 +436,7 @@ template <int N, int M, int D, class Part> __device__ __forceinline__ void few_a
 // of the first cut does all runs).
 template <int D, int NT> struct FewJoin { static constexpr int kRuns = 16 * NT * D / 256, kWaves = kRuns > 8 ? kRuns : 16 / kRuns * kRuns, kThreads = 64 * kWaves; };
 template <typename T, int D, int NT> __device__ __forceinline__ void paged_few_join(const PagedArgs& a, FewLine<NT>& line, int log_groups, int b) {
-  constexpr int M = 16 * NT, R = FewJoin<D, NT>::kRuns, W = FewJoin<D, NT>::kWaves;
+  constexpr int M = 16 * NT, W = FewJoin<D, NT>::kWaves;
   constexpr int64_t kFloats = FewPart<D, NT>::kFloats;
   __shared__ FewSum sums[W][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));

@@ -3,8 +3,8 @@
 // A workgroup has 128 rows of one request and key head, 32 to a wavefront, and walks the keys that they see 64 at a time: keys
 // and values by direct loads into LDS, the next 64 in flight to the other half while these are worked on, one
 // barrier a step.  Both dots are v_mfma_f32_32x32x16.  A tile of more than an even share of the work is split over workgroups
-// by its keys, and paged_mixed_join_kernel adds the parts in their order.  925 TFLOP/s at D 128 (8 chunks of 1 to 1024 tokens behind up to 12000 keys, 32 / 8
-// heads, 359 us; the card's rate of a bf16 product of 8192^3 is 1205), 600 at D 64 (4 prompts of 2048 x 16 heads, 57.3 us).
+// by its keys, and paged_mixed_join_kernel adds the parts in their order.  850 to 930 TFLOP/s at D 128, by the card and its clock (8 chunks of 1 to 1024 tokens behind up to
+// 12000 keys, 32 / 8 heads, 357 to 390 us; a bf16 product of 8192^3 1205 to 1240), 575 to 605 at D 64 (4 prompts of 2048 x 16 heads, 57 to 60 us).
 #pragma once
 #include <algorithm>
 
@@ -400,7 +400,7 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile(const Pa
         sum += e;
       }
     l += sum;
-    u32x4 pb[4];
+    u32x4 pb[4];      // rounded to T for the second dot alone: half a step of each weight; their sum is of them unrounded
 #pragma unroll
     for (int k = 0; k < 4; ++k)
 #pragma unroll
@@ -495,8 +495,10 @@ template <typename T, int D> __device__ __forceinline__ void paged_tile_join(con
   }
 }
 
-// Requests of few rows and of many in one launch, and one that joins the parts of both: the former read memory while the latter keep the
-// matrix unit busy, and where there are none of them (whole prompts) they cost no launches of their own.  Four workgroups to a CU up to head dim
+// Requests of few rows and of many in one launch, and one that joins the parts of both: where there are none of one kind (whole prompts) it costs no
+// launches of its own.  Those of few rows are numbered behind all tiles and begin as these run out, so that one kind reads memory while the other keeps
+// the matrix unit busy at the tiles' end alone (512 tokens behind 32256 keys and 100 single ones behind 4095: 494 us, where the products take
+// 226 and the reading 254; by turns of eight both ended up on shader engines of their own, chunks 378 -> 501).  Four workgroups to a CU up to head dim
 // 64 (prompts of 2048 rows x 16 heads of 64: 60.5 us, 66.6 with three); beyond, two is what the LDS holds.
 template <typename T, int D, int NT> __global__ __launch_bounds__(256, (D <= 64 && NT == 1 ? 4 : 2)) void paged_mixed_kernel(const PagedArgs a) {
   __shared__ __align__(1024) union { FewLds<D, NT, 4> few; TileShared<D> tile; } lds;
