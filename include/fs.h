@@ -153,7 +153,10 @@ typedef enum {
                                 ops that read their results */
   FS_SCHED_BLOCK_TABLES = 7, /* the operators around a paged cache: fs_plan_create_block_tables, */
   FS_SCHED_ROTARY = 8,       /* fs_plan_create_rotary, */
-  FS_SCHED_PAGED_ATTENTION = 9 /* fs_plan_create_paged_attention */
+  FS_SCHED_PAGED_ATTENTION = 9, /* fs_plan_create_paged_attention */
+  FS_SCHED_CACHE_STORE8 = 10, /* ... in 8 bits: fs_plan_create_cache_store8, */
+  FS_SCHED_CACHE_READ8 = 11,  /* fs_plan_create_cache_read8, */
+  FS_SCHED_PAGED_ATTENTION8 = 12 /* fs_plan_create_paged_attention8 */
 } fs_schedule;
 
 /* Build a plan from a fusion group.
@@ -508,6 +511,63 @@ typedef struct {
   double scale;                    /* finite */
 } fs_paged_attention_desc;
 fs_status fs_plan_create_paged_attention(const fs_paged_attention_desc* desc, int64_t* partial_bytes, fs_plan** out);
+
+/* ---- The paged cache in 8 bits ------------------------------------------------------------
+ * Keys and values are held as codes of one byte, in a cache laid out as above (strides in codes, multiples of 16), with a scale, a 32-bit number, for each block of tokens
+ * and head: k_scales and v_scales f32 [blocks, kv_heads], dense.  A code c of block b and head h stands for c * scales[b, h].  FS_CODE_E4M3: four exponent
+ * bits, three behind the first one, up to 448, NaN 0x7f and 0xff, no infinity.  FS_CODE_INT8: -127 to 127.  block_size 8 to 1024. */
+typedef enum { FS_CODE_E4M3 = 0, FS_CODE_INT8 = 1 } fs_code;
+
+/* New keys and values quantised as they are written.  Request b's new tokens are rows starts[b] .. starts[b+1]-1 of k and v and the last of
+ * its lengths[b] tokens (what block tables give, and attention takes).  For every block that they touch and every head
+ *     need = the least power of two s, 2^-126 or more, with |x| <= largest code * s for the block's new numbers x
+ *     scale = need, where the block's first token is new; else the larger of need and the scale from before, up to a power of two
+ *     codes of the block's tokens from before, where that scale has changed: c * before / scale; of the new ones: x / scale; rounded to the
+ *     nearest, the even one of two
+ * Powers of two: c * scale is exact in every type, a block that grows loses of e4m3 codes only what falls below their least numbers, and of whole numbers, over all
+ * its growth, less than one step of its last scale.  Numbers whose code would stand for an infinity of dtype are cut to the largest that does not.  A
+ * new number that is infinite or NaN, or such a scale from before, makes the scale NaN: nothing of that block and head is a number then, until
+ * the block begins anew.
+ *   inputs    k, v [tokens, kv_heads, head_dim], tables i32 [requests, table_blocks], lengths i32 [requests], starts i32 [requests+1]
+ *   outputs   k_cache, v_cache, k_scales, v_scales (read and written)
+ * Nothing is written for rows of no request or before a request's first token, for blocks outside [0, blocks), and in other places of a block than those of the request's tokens.  Two
+ * requests that write to one block leave it undefined.
+ * dtype FS_F32, FS_F16 or FS_BF16, head_dim a multiple of 16 up to 512, rows of k and v on 16 bytes.
+ * Errors: FS_ERR_INVALID, FS_ERR_UNSUPPORTED (a head_dim, stride or block_size that no kernel takes), FS_ERR_NOMEM. */
+typedef struct {
+  int32_t dtype, code;             /* of k and v; fs_code */
+  int32_t requests, tokens, kv_heads, head_dim;
+  int32_t blocks, block_size, table_blocks;
+  int32_t reserved;                /* must be 0 */
+  int64_t k_stride, v_stride;      /* from token to token, 0: dense */
+  int64_t block_stride, head_stride, slot_stride;
+} fs_cache8_desc;
+fs_status fs_plan_create_cache_store8(const fs_cache8_desc* desc, fs_plan** out);
+
+/* ... and read back: rows starts[b] .. starts[b+1]-1 of k and v get the last so many of request b's lengths[b] tokens, c * scale rounded to dtype.
+ *   inputs    k_cache, v_cache, k_scales, v_scales, tables, lengths, starts
+ *   outputs   k, v [tokens, kv_heads, head_dim]
+ * Tokens in blocks outside [0, blocks), and rows before a request's first token, are zeros; rows outside every request are left as they were.
+ * Limits and errors as above. */
+fs_status fs_plan_create_cache_read8(const fs_cache8_desc* desc, fs_plan** out);
+
+/* Attention of new tokens over the cache in 8 bits: fs_plan_create_paged_attention with the numbers that the codes stand for as keys and values.
+ *   inputs    q, k_cache, v_cache, k_scales, v_scales, tables, lengths, starts
+ *   outputs   out; with log_sum_exp also lse; with partial_bytes not 0 also the partial results
+ * Any scales are taken: values (and where a request may have more than 32 rows, keys) whose scale is no power of two may be rounded to dtype, where 16-bit keys and values had been rounded
+ * before; numbers beyond its range may count as infinities.  What is said there of masks, blocks outside, lengths, rows of no request and NaN holds here, for scales too: one of
+ * a block that a row does not see never reaches it. block_size 8 to 1024, strides of the cache multiples of 16 codes. */
+typedef struct {
+  int32_t dtype, code;             /* FS_F16 or FS_BF16: q, out; fs_code: the caches */
+  int32_t requests, tokens, q_heads, kv_heads, head_dim;
+  int32_t blocks, block_size, table_blocks;
+  int32_t causal, window;
+  int32_t max_new, log_sum_exp;
+  int64_t q_stride, out_stride;
+  int64_t block_stride, head_stride, slot_stride;
+  double scale;
+} fs_paged_attention8_desc;
+fs_status fs_plan_create_paged_attention8(const fs_paged_attention8_desc* desc, int64_t* partial_bytes, fs_plan** out);
 
 /* Measurement aid: plain streaming copy of `bytes` (multiple of 16) from src to dst,
  * both DEVICE pointers, 16-byte aligned, on `hip_stream`.  Gives the achievable HBM

@@ -22,9 +22,10 @@ FS_OK, FS_ERR_INVALID, FS_ERR_UNSUPPORTED, FS_ERR_LDS, FS_ERR_HIP, FS_ERR_NOMEM 
 STATUS_NAMES = ["FS_OK", "FS_ERR_INVALID", "FS_ERR_UNSUPPORTED", "FS_ERR_LDS", "FS_ERR_HIP", "FS_ERR_NOMEM"]
 FS_MODE_STITCHED, FS_MODE_PER_OP, FS_MODE_STITCHED_PREBUILT, FS_MODE_STITCHED_GENERATED = 0, 1, 2, 3
 SCHEDULE_NAMES = ["per_op", "row", "row_col", "bdot_softmax", "elementwise", "block_dot", "two_step", "block_tables", "rotary",
-                  "paged_attention"]
+                  "paged_attention", "cache_store8", "cache_read8", "paged_attention8"]
 
 DTYPES = {"f32": 0, "f16": 1, "bf16": 2}
+CODES = {"e4m3": 0, "int8": 1}
 OPKINDS = {name: i for i, name in enumerate((
     "parameter", "constant", "add", "subtract", "multiply", "divide", "maximum", "negate",
     "exp", "log", "tanh", "rsqrt", "sqrt", "convert", "broadcast", "reduce_sum", "reduce_max",
@@ -63,6 +64,17 @@ class fs_rotary_desc(C.Structure):
 class fs_paged_attention_desc(C.Structure):
     _fields_ = ([(n, C.c_int32) for n in ("dtype", "requests", "tokens", "q_heads", "kv_heads", "head_dim", "blocks", "block_size", "table_blocks",
                                           "causal", "window", "max_new", "log_sum_exp", "reserved")] +
+                [(n, C.c_int64) for n in ("q_stride", "out_stride", "block_stride", "head_stride", "slot_stride")] + [("scale", C.c_double)])
+
+
+class fs_cache8_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "code", "requests", "tokens", "kv_heads", "head_dim", "blocks", "block_size", "table_blocks", "reserved")] +
+                [(n, C.c_int64) for n in ("k_stride", "v_stride", "block_stride", "head_stride", "slot_stride")])
+
+
+class fs_paged_attention8_desc(C.Structure):
+    _fields_ = ([(n, C.c_int32) for n in ("dtype", "code", "requests", "tokens", "q_heads", "kv_heads", "head_dim", "blocks", "block_size", "table_blocks",
+                                          "causal", "window", "max_new", "log_sum_exp")] +
                 [(n, C.c_int64) for n in ("q_stride", "out_stride", "block_stride", "head_stride", "slot_stride")] + [("scale", C.c_double)])
 
 
@@ -158,6 +170,11 @@ def lib():
         L.fs_rotary_frequencies.restype = i32
         L.fs_plan_create_paged_attention.argtypes = [C.POINTER(fs_paged_attention_desc), C.POINTER(i64), C.POINTER(vp)]
         L.fs_plan_create_paged_attention.restype = i32
+        for f in (L.fs_plan_create_cache_store8, L.fs_plan_create_cache_read8):
+            f.argtypes = [C.POINTER(fs_cache8_desc), C.POINTER(vp)]
+            f.restype = i32
+        L.fs_plan_create_paged_attention8.argtypes = [C.POINTER(fs_paged_attention8_desc), C.POINTER(i64), C.POINTER(vp)]
+        L.fs_plan_create_paged_attention8.restype = i32
         _native = _launch_calls(L)
         _lib = L
     return _lib
@@ -304,6 +321,41 @@ def fs_plan_create_paged_attention(dtype, requests, tokens, q_heads, kv_heads, h
                                 int(lse), 0, q_stride, out_stride, block_stride, head_stride, slot_stride, scale)
     nbytes, out = C.c_int64(), C.c_void_p()
     _check(lib().fs_plan_create_paged_attention(C.byref(d), C.byref(nbytes), C.byref(out)))
+    return out.value, nbytes.value
+
+
+# ---- the paged cache in 8 bits; code: "e4m3" or "int8"
+
+def _cache8(create, dtype, code, requests, tokens, kv_heads, head_dim, blocks, block_size, table_blocks, k_stride, v_stride, block_stride, head_stride, slot_stride):
+    d = fs_cache8_desc(DTYPES[dtype], CODES[code], requests, tokens, kv_heads, head_dim, blocks, block_size, table_blocks, 0, k_stride, v_stride, block_stride, head_stride, slot_stride)
+    out = C.c_void_p()
+    _check(create(C.byref(d), C.byref(out)))
+    return out.value
+
+
+def fs_plan_create_cache_store8(dtype, code, requests, tokens, kv_heads, head_dim, blocks, block_size, table_blocks, k_stride=0, v_stride=0,
+                                block_stride=0, head_stride=0, slot_stride=0):
+    """-> plan handle.  Inputs k, v, tables, lengths, starts (int32); outputs k_cache, v_cache (bytes), k_scales, v_scales (float32), read and
+    written.  Strides of k and v in elements from token to token, of the caches in codes; 0: dense."""
+    return _cache8(lib().fs_plan_create_cache_store8, dtype, code, requests, tokens, kv_heads, head_dim, blocks, block_size, table_blocks, k_stride, v_stride,
+                   block_stride, head_stride, slot_stride)
+
+
+def fs_plan_create_cache_read8(dtype, code, requests, tokens, kv_heads, head_dim, blocks, block_size, table_blocks, k_stride=0, v_stride=0,
+                               block_stride=0, head_stride=0, slot_stride=0):
+    """-> plan handle.  Inputs k_cache, v_cache, k_scales, v_scales, tables, lengths, starts; outputs k, v of `dtype`."""
+    return _cache8(lib().fs_plan_create_cache_read8, dtype, code, requests, tokens, kv_heads, head_dim, blocks, block_size, table_blocks, k_stride, v_stride,
+                   block_stride, head_stride, slot_stride)
+
+
+def fs_plan_create_paged_attention8(dtype, code, requests, tokens, q_heads, kv_heads, head_dim, blocks, block_size, table_blocks, scale, causal=True,
+                                    window=0, max_new=0, lse=False, q_stride=0, out_stride=0, block_stride=0, head_stride=0, slot_stride=0):
+    """-> (plan handle, bytes of the partial results, as of fs_plan_create_paged_attention).  Inputs q, k_cache, v_cache, k_scales, v_scales, tables,
+    lengths, starts; outputs out, with lse also the log-sum-exp (float32)."""
+    d = fs_paged_attention8_desc(DTYPES[dtype], CODES[code], requests, tokens, q_heads, kv_heads, head_dim, blocks, block_size, table_blocks, int(causal), window,
+                                 max_new, int(lse), q_stride, out_stride, block_stride, head_stride, slot_stride, scale)
+    nbytes, out = C.c_int64(), C.c_void_p()
+    _check(lib().fs_plan_create_paged_attention8(C.byref(d), C.byref(nbytes), C.byref(out)))
     return out.value, nbytes.value
 
 
@@ -494,6 +546,22 @@ class Plan:
     def paged_attention(cls, *args, **kwargs):
         """fs_plan_create_paged_attention -> (plan, bytes of the buffer it takes as its last output, 0: none)."""
         h, nbytes = fs_plan_create_paged_attention(*args, **kwargs)
+        return cls(None, _handle=h), nbytes
+
+    @classmethod
+    def cache_store8(cls, *args, **kwargs):
+        """fs_plan_create_cache_store8 -> plan."""
+        return cls(None, _handle=fs_plan_create_cache_store8(*args, **kwargs))
+
+    @classmethod
+    def cache_read8(cls, *args, **kwargs):
+        """fs_plan_create_cache_read8 -> plan."""
+        return cls(None, _handle=fs_plan_create_cache_read8(*args, **kwargs))
+
+    @classmethod
+    def paged_attention8(cls, *args, **kwargs):
+        """fs_plan_create_paged_attention8 -> (plan, bytes of the buffer it takes as its last output, 0: none)."""
+        h, nbytes = fs_plan_create_paged_attention8(*args, **kwargs)
         return cls(None, _handle=h), nbytes
 
     @classmethod

@@ -552,7 +552,10 @@ fs_status fs::enqueue_plan(fs_plan* p, const void* const* inputs, void* const* o
       case FS_SCHED_TWO_STEP: rc = fs::two_step_launch(p->two_step, inputs, outputs, n_out - 1, outputs[n_out - 1], hip_stream, &err); break;
       case FS_SCHED_BLOCK_TABLES:
       case FS_SCHED_ROTARY:
-      case FS_SCHED_PAGED_ATTENTION: rc = fs::paged_launch(p->paged, inputs, outputs, hip_stream, &err); break;
+      case FS_SCHED_PAGED_ATTENTION:
+      case FS_SCHED_CACHE_STORE8:
+      case FS_SCHED_CACHE_READ8:
+      case FS_SCHED_PAGED_ATTENTION8: rc = fs::paged_launch(p->paged, inputs, outputs, hip_stream, &err); break;
       default: rc = fs::per_op_launch(p->graph, p->per_op, inputs, outputs, workspace, hip_stream, &err); break;
     }
     if (rc != 0) return set_error(FS_ERR_HIP, err);

@@ -1,0 +1,90 @@
+// Codes of a paged cache in 8 bits on the device: e4m3 (four exponent bits, three behind the first one, up to 448, NaN 0x7f and 0xff, no
+// infinity) and whole numbers from -127 to 127.
+#pragma once
+#include "dev_common.h"
+#include "paged.h"
+
+namespace fs {
+
+struct E4m3 {
+  // The largest number of T that a code stands for, the scale being the one that a block with T's largest numbers gets: beyond, rounding could end at infinity.
+  template <typename T> static constexpr float kMost = __is_same(T, f16_t) ? 61440.f : 0x1.ep+127f;
+  // the least power of two that reaches x with a code of 448 = 1.75 * 2^8; 0 and subnormal numbers: one of -126 and less
+  static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 135 + ((as_u32(x) & 0x7fffffu) > 0x600000u); }
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) {
+    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+  }
+  static __device__ __forceinline__ void unpack(uint32_t c, float (&x)[4]) {
+    const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
+    x[0] = lo[0]; x[1] = lo[1]; x[2] = hi[0]; x[3] = hi[1];
+  }
+};
+
+struct Int8 {
+  template <typename T> static constexpr float kMost = __is_same(T, f16_t) ? 64512.f : 0x1.f8p+127f;
+  // 127 = 1.984375 * 2^6
+  static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 133 + ((as_u32(x) & 0x7fffffu) > 0x7e0000u); }
+  // 1.5 * 2^23 more leaves the nearest whole number, the even one of two, in the number's last bits
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) {
+    const uint32_t w0 = as_u32(a + 0x1.8p23f), w1 = as_u32(b + 0x1.8p23f), w2 = as_u32(c + 0x1.8p23f), w3 = as_u32(d + 0x1.8p23f);
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w3, w2, 0x0c0c0400u), __builtin_amdgcn_perm(w1, w0, 0x0c0c0400u), 0x05040100u);
+  }
+  static __device__ __forceinline__ void unpack(uint32_t c, float (&x)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(c >> (8 * i));
+  }
+};
+
+// Eight codes as numbers of T for the matrix unit: as they stand (plain: exact in both types), or the first four times s0 and the others times s1, rounded
+// to T (scaled).  One instruction makes two numbers of e4m3 codes and takes a power of two with it: its scales are powers of two (power_of), and what
+// is left of a scale (rest_of: 1 for what the store writes) goes into the dot's other operand or its result.  Whole numbers are multiplied in fp32.
+__device__ __forceinline__ float power_of(float s) {
+  const uint32_t e = as_u32(s) & 0x7f800000u;
+  return e == 0 || e == 0x7f800000u ? 1.f : as_f32(e);
+}
+__device__ __forceinline__ float rest_of(float s) {
+  const uint32_t e = as_u32(s) & 0x7f800000u;
+  return e == 0 || e == 0x7f800000u ? s : as_f32((as_u32(s) & 0x807fffffu) | 0x3f800000u);
+}
+
+template <class Code, typename T> struct Numbers;
+template <typename T> struct Numbers<E4m3, T> {
+  template <bool HI> static __device__ __forceinline__ uint32_t two(uint32_t c, float s) {
+    if constexpr (__is_same(T, bf16_t)) return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c, s, HI));
+    else return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c, s, HI));
+  }
+  static __device__ __forceinline__ u32x4 scaled(u32x2 c, float s0, float s1) {
+    return u32x4{two<false>(c[0], s0), two<true>(c[0], s0), two<false>(c[1], s1), two<true>(c[1], s1)};
+  }
+  static __device__ __forceinline__ u32x4 plain(u32x2 c) { return scaled(c, 1.f, 1.f); }
+};
+template <typename T> struct Numbers<Int8, T> {
+  static __device__ __forceinline__ uint32_t two(float a, float b) {
+    if constexpr (__is_same(T, bf16_t)) return pack2_bf16(a, b);
+    else return pack2_f16(a, b);
+  }
+  static __device__ __forceinline__ u32x4 scaled(u32x2 c, float s0, float s1) {
+    float x[4], y[4];
+    Int8::unpack(c[0], x);
+    Int8::unpack(c[1], y);
+    return u32x4{two(x[0] * s0, x[1] * s0), two(x[2] * s0, x[3] * s0), two(y[0] * s1, y[1] * s1), two(y[2] * s1, y[3] * s1)};
+  }
+  static __device__ __forceinline__ u32x4 plain(u32x2 c) {
+    if constexpr (__is_same(T, bf16_t)) return scaled(c, 1.f, 1.f);
+    else {
+      // bytes without their sign, 128 more each, as the last bits of 1024 + them; less 1152
+      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+      const h2 off = {(_Float16)1152.f, (_Float16)1152.f};
+      u32x4 out;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t w = __builtin_amdgcn_perm(0x64646464u, c[i / 2] ^ 0x80808080u, i & 1 ? 0x04030402u : 0x04010400u);
+        out[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, w) - off);
+      }
+      return out;
+    }
+  }
+};
+
+}  // namespace fs

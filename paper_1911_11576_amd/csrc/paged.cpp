@@ -87,6 +87,127 @@ template <class Build> fs_status create(fs_plan** out, const char* what, Build b
   return FS_OK;
 }
 
+bool known_code(int code) { return code == FS_CODE_E4M3 || code == FS_CODE_INT8; }
+
+// What the kernels of a cache in 8 bits take: four neighbouring keys in one block, rows on 16 bytes.
+bool codes_fit(const CacheLayout& c, int64_t block_size, std::string* err) {
+  if (block_size < 8) { *err = "block_size must be at least 8"; return false; }
+  for (int64_t n : {c.block, c.head, c.slot})
+    if (n % 16) { *err = "strides of the cache must be multiples of 16 codes"; return false; }
+  return true;
+}
+
+// Attention over a cache of numbers of the type (code -1) or of codes of 8 bits.
+fs_status create_attention(const char* what, const fs_paged_attention_desc& desc, int code, int64_t* partial_bytes, fs_plan** out) {
+  if (!partial_bytes) return invalid(what, "partial_bytes is NULL");
+  *partial_bytes = 0;
+  return create(out, what, [&](fs_plan* p, int* status, std::string* err) {
+    fs::PagedAttnSpec& s = p->paged.attn;
+    s.d = desc;
+    s.code = code;
+    fs_paged_attention_desc& d = s.d;
+    const bool coded = code >= 0;
+    const int64_t e = coded ? 1 : 2;      // bytes of the cache's elements
+    if (d.reserved) { *err = "reserved must be 0"; return false; }
+    if (d.dtype != FS_F32 && d.dtype != FS_F16 && d.dtype != FS_BF16) { *err = "unknown dtype"; return false; }
+    if (d.requests < 0 || d.requests > 65536) { *err = "requests out of range [0,65536]"; return false; }
+    if (d.q_heads < 1 || d.kv_heads < 1 || d.q_heads % d.kv_heads || d.q_heads > 65536) { *err = "q_heads must be a multiple of kv_heads, both above 0 and up to 65536"; return false; }
+    if (d.tokens < 0 || (int64_t)d.tokens * d.q_heads > kMostTokens) { *err = "tokens below 0, or tokens * q_heads beyond 2^30"; return false; }
+    if (d.head_dim < 1) { *err = "head_dim must be above 0"; return false; }
+    if (d.blocks < 0 || d.table_blocks < 0) { *err = "negative number of blocks"; return false; }
+    if (!blocks_fit(d.blocks, d.block_size, &s.cache.shift, err) || !blocks_fit(d.table_blocks, d.block_size, &s.cache.shift, err)) return false;
+    if ((d.causal | 1) != 1 || (d.log_sum_exp | 1) != 1) { *err = "causal and log_sum_exp are 0 or 1"; return false; }
+    if (d.window < 0 || (d.window && !d.causal)) { *err = "window below 0, or without causal"; return false; }
+    if (d.max_new < 0) { *err = "max_new below 0"; return false; }
+    if (!std::isfinite((float)(d.scale * 1.4426950408889634))) { *err = "scale must be finite in fp32"; return false; }
+    const int64_t t = d.tokens, dim = d.head_dim, row = d.q_heads * dim;
+    if (!token_stride(&d.q_stride, d.q_heads, dim, "q_stride", err) || !token_stride(&d.out_stride, d.q_heads, dim, "out_stride", err)) return false;
+    int64_t cache_bytes = 0;
+    const int shift = s.cache.shift;
+    if (!cache_layout(d.blocks, d.kv_heads, d.block_size, dim, d.block_stride, d.head_stride, d.slot_stride, e, &s.cache, &cache_bytes, err)) return false;
+    s.cache.shift = shift;
+    *status = FS_ERR_UNSUPPORTED;
+    if (d.dtype == FS_F32) { *err = "f16 and bf16 alone"; return false; }
+    if (dim != 32 && dim != 64 && dim != 96 && dim != 128) { *err = "head_dim must be 32, 64, 96 or 128"; return false; }
+    for (int64_t n : {d.q_stride, d.out_stride, s.cache.block, s.cache.head, s.cache.slot})
+      if (n % 8) { *err = "strides must be multiples of 8 elements"; return false; }
+    if (coded && !codes_fit(s.cache, d.block_size, err)) return false;
+    s.share = d.q_heads / d.kv_heads;
+    if (!fs::paged_attn_plan(&s, &p->n_kernels, &p->lds_bytes, err)) return false;
+    fs::PagedPlan& g = p->paged;
+    const int64_t b = t ? d.requests : 0;        // (no rows: nothing is launched)
+    const bool cached = t && d.requests;
+    const int64_t scales = 4ll * d.blocks * d.kv_heads;
+    g.kind = coded ? FS_SCHED_PAGED_ATTENTION8 : FS_SCHED_PAGED_ATTENTION;
+    g.in = {{"q", rows_bytes(t, d.q_stride, row, 2), -1}, {"k_cache", cached ? cache_bytes : 0, -1}, {"v_cache", cached ? cache_bytes : 0, -1}};
+    if (coded) {
+      g.in.push_back({"k_scales", cached ? scales : 0, -1});
+      g.in.push_back({"v_scales", cached ? scales : 0, -1});
+    }
+    g.in.push_back({"tables", 4 * b * d.table_blocks, -1});
+    g.in.push_back({"lengths", 4 * b, -1});
+    g.in.push_back({"starts", b ? 4 * (b + 1) : 0, -1});
+    g.out = {{"out", rows_bytes(t, d.out_stride, row, 2), -1}};
+    if (d.log_sum_exp) g.out.push_back({"lse", 4 * t * d.q_heads, -1});
+    if (s.partial_bytes) g.out.push_back({"partials", s.partial_bytes, -1});
+    const int64_t keys = std::min<int64_t>((int64_t)d.requests * d.table_blocks * d.block_size, (int64_t)d.blocks * d.block_size);
+    g.bytes = 4 * t * row + 2 * e * keys * d.kv_heads * dim + (coded ? 8 * (keys >> shift) * d.kv_heads : 0) + 4ll * d.requests * (d.table_blocks + 2) + (d.log_sum_exp ? 4 * t * d.q_heads : 0);
+    p->description = fs::paged_attn_describe(s);
+    *partial_bytes = s.partial_bytes;
+    return true;
+  });
+}
+
+// The store into a cache in 8 bits, and the reading back.
+fs_status create_cache8(const char* what, const fs_cache8_desc* desc, bool store, fs_plan** out) {
+  if (out) *out = nullptr;
+  if (!desc) return invalid(what, "desc is NULL");
+  return create(out, what, [&](fs_plan* p, int* status, std::string* err) {
+    fs::Cache8Spec& s = p->paged.cache8;
+    s.d = *desc;
+    fs_cache8_desc& d = s.d;
+    if (d.reserved) { *err = "reserved must be 0"; return false; }
+    if (d.dtype != FS_F32 && d.dtype != FS_F16 && d.dtype != FS_BF16) { *err = "unknown dtype"; return false; }
+    if (!known_code(d.code)) { *err = "unknown code"; return false; }
+    if (d.requests < 0 || d.requests > 65536) { *err = "requests out of range [0,65536]"; return false; }
+    if (d.tokens < 0 || d.tokens > kMostTokens) { *err = "tokens out of range [0,2^30]"; return false; }
+    if (d.kv_heads < 1 || d.kv_heads > 65536) { *err = "kv_heads out of range [1,65536]"; return false; }
+    if (d.head_dim < 1) { *err = "head_dim must be above 0"; return false; }
+    if (d.blocks < 0 || d.table_blocks < 0) { *err = "negative number of blocks"; return false; }
+    if (!blocks_fit(d.blocks, d.block_size, &s.cache.shift, err) || !blocks_fit(d.table_blocks, d.block_size, &s.cache.shift, err)) return false;
+    const int64_t t = d.tokens, dim = d.head_dim, row = d.kv_heads * dim, e = size_of(d.dtype);
+    if (!token_stride(&d.k_stride, d.kv_heads, dim, "k_stride", err) || !token_stride(&d.v_stride, d.kv_heads, dim, "v_stride", err)) return false;
+    int64_t cache_bytes = 0;
+    const int shift = s.cache.shift;
+    if (!cache_layout(d.blocks, d.kv_heads, d.block_size, dim, d.block_stride, d.head_stride, d.slot_stride, 1, &s.cache, &cache_bytes, err)) return false;
+    s.cache.shift = shift;
+    *status = FS_ERR_UNSUPPORTED;
+    if (dim % 16 || dim > 512) { *err = "head_dim must be a multiple of 16 up to 512"; return false; }
+    if (d.k_stride * e % 16 || d.v_stride * e % 16) { *err = "rows of k and v must lie on 16 bytes"; return false; }
+    if (!codes_fit(s.cache, d.block_size, err)) return false;
+    fs::cache8_geometry(&s, store);
+    fs::PagedPlan& g = p->paged;
+    const int64_t b = t ? d.requests : 0;        // (no rows: nothing is launched)
+    const bool any = t && d.requests;
+    const int64_t scales = 4ll * d.blocks * d.kv_heads;
+    g.kind = store ? FS_SCHED_CACHE_STORE8 : FS_SCHED_CACHE_READ8;
+    const std::vector<fs::PagedBuffer> rows = {{"k", any ? rows_bytes(t, d.k_stride, row, e) : 0, -1}, {"v", any ? rows_bytes(t, d.v_stride, row, e) : 0, -1}};
+    const std::vector<fs::PagedBuffer> cache = {{"k_cache", any ? cache_bytes : 0, -1}, {"v_cache", any ? cache_bytes : 0, -1}, {"k_scales", any ? scales : 0, -1}, {"v_scales", any ? scales : 0, -1}};
+    g.in = store ? rows : cache;
+    g.in.push_back({"tables", 4 * b * d.table_blocks, -1});
+    g.in.push_back({"lengths", 4 * b, -1});
+    g.in.push_back({"starts", b ? 4 * (b + 1) : 0, -1});
+    g.out = store ? cache : rows;
+    const int64_t touched = std::min<int64_t>((t >> shift) + 2 * b, d.blocks);
+    g.bytes = 2 * t * row * (e + 1) + 8 * touched * d.kv_heads + 4 * (2 * b + touched);
+    if (store) p->lds_bytes = 16;
+    else p->lds_bytes = 768;
+    p->description = store ? numbers("cache_store8[GRID-CTA,WARP] wavefronts to a block and head=%lld; cta_num=%lld, cta_size=256", s.waves, s.grid)
+                           : numbers("cache_read8[GRID-CTA,THREAD] rows=%lld; cta_num=%lld, cta_size=256", s.groups, s.grid);
+    return true;
+  });
+}
+
 }  // namespace
 
 extern "C" {
@@ -211,53 +332,22 @@ fs_status fs_plan_create_paged_attention(const fs_paged_attention_desc* desc, in
   const char* what = "fs_plan_create_paged_attention";
   if (out) *out = nullptr;
   if (!desc) return invalid(what, "desc is NULL");
-  if (!partial_bytes) return invalid(what, "partial_bytes is NULL");
-  *partial_bytes = 0;
-  return create(out, what, [&](fs_plan* p, int* status, std::string* err) {
-    fs::PagedAttnSpec& s = p->paged.attn;
-    s.d = *desc;
-    fs_paged_attention_desc& d = s.d;
-    if (d.reserved) { *err = "reserved must be 0"; return false; }
-    if (d.dtype != FS_F32 && d.dtype != FS_F16 && d.dtype != FS_BF16) { *err = "unknown dtype"; return false; }
-    if (d.requests < 0 || d.requests > 65536) { *err = "requests out of range [0,65536]"; return false; }
-    if (d.q_heads < 1 || d.kv_heads < 1 || d.q_heads % d.kv_heads || d.q_heads > 65536) { *err = "q_heads must be a multiple of kv_heads, both above 0 and up to 65536"; return false; }
-    if (d.tokens < 0 || (int64_t)d.tokens * d.q_heads > kMostTokens) { *err = "tokens below 0, or tokens * q_heads beyond 2^30"; return false; }
-    if (d.head_dim < 1) { *err = "head_dim must be above 0"; return false; }
-    if (d.blocks < 0 || d.table_blocks < 0) { *err = "negative number of blocks"; return false; }
-    if (!blocks_fit(d.blocks, d.block_size, &s.cache.shift, err) || !blocks_fit(d.table_blocks, d.block_size, &s.cache.shift, err)) return false;
-    if ((d.causal | 1) != 1 || (d.log_sum_exp | 1) != 1) { *err = "causal and log_sum_exp are 0 or 1"; return false; }
-    if (d.window < 0 || (d.window && !d.causal)) { *err = "window below 0, or without causal"; return false; }
-    if (d.max_new < 0) { *err = "max_new below 0"; return false; }
-    if (!std::isfinite((float)(d.scale * 1.4426950408889634))) { *err = "scale must be finite in fp32"; return false; }
-    const int64_t t = d.tokens, dim = d.head_dim, row = d.q_heads * dim;
-    if (!token_stride(&d.q_stride, d.q_heads, dim, "q_stride", err) || !token_stride(&d.out_stride, d.q_heads, dim, "out_stride", err)) return false;
-    int64_t cache_bytes = 0;
-    const int shift = s.cache.shift;
-    if (!cache_layout(d.blocks, d.kv_heads, d.block_size, dim, d.block_stride, d.head_stride, d.slot_stride, 2, &s.cache, &cache_bytes, err)) return false;
-    s.cache.shift = shift;
-    *status = FS_ERR_UNSUPPORTED;
-    if (d.dtype == FS_F32) { *err = "f16 and bf16 alone"; return false; }
-    if (dim != 32 && dim != 64 && dim != 96 && dim != 128) { *err = "head_dim must be 32, 64, 96 or 128"; return false; }
-    for (int64_t n : {d.q_stride, d.out_stride, s.cache.block, s.cache.head, s.cache.slot})
-      if (n % 8) { *err = "strides must be multiples of 8 elements"; return false; }
-    s.share = d.q_heads / d.kv_heads;
-    if (!fs::paged_attn_plan(&s, &p->n_kernels, &p->lds_bytes, err)) return false;
-    fs::PagedPlan& g = p->paged;
-    const int64_t b = t ? d.requests : 0;        // (no rows: nothing is launched)
-    const bool cached = t && d.requests;
-    g.kind = FS_SCHED_PAGED_ATTENTION;
-    g.in = {{"q", rows_bytes(t, d.q_stride, row, 2), -1}, {"k_cache", cached ? cache_bytes : 0, -1}, {"v_cache", cached ? cache_bytes : 0, -1},
-            {"tables", 4 * b * d.table_blocks, -1}, {"lengths", 4 * b, -1}, {"starts", b ? 4 * (b + 1) : 0, -1}};
-    g.out = {{"out", rows_bytes(t, d.out_stride, row, 2), -1}};
-    if (d.log_sum_exp) g.out.push_back({"lse", 4 * t * d.q_heads, -1});
-    if (s.partial_bytes) g.out.push_back({"partials", s.partial_bytes, -1});
-    const int64_t keys = std::min<int64_t>((int64_t)d.requests * d.table_blocks * d.block_size, (int64_t)d.blocks * d.block_size);
-    g.bytes = 4 * t * row + 4 * keys * d.kv_heads * dim + 4ll * d.requests * (d.table_blocks + 2) + (d.log_sum_exp ? 4 * t * d.q_heads : 0);
-    p->description = fs::paged_attn_describe(s);
-    *partial_bytes = s.partial_bytes;
-    return true;
-  });
+  return create_attention(what, *desc, -1, partial_bytes, out);
 }
+
+fs_status fs_plan_create_paged_attention8(const fs_paged_attention8_desc* desc, int64_t* partial_bytes, fs_plan** out) {
+  const char* what = "fs_plan_create_paged_attention8";
+  if (out) *out = nullptr;
+  if (!desc) return invalid(what, "desc is NULL");
+  if (!known_code(desc->code)) return invalid(what, "unknown code");
+  const fs_paged_attention8_desc& d = *desc;
+  const fs_paged_attention_desc same = {d.dtype, d.requests, d.tokens, d.q_heads, d.kv_heads, d.head_dim, d.blocks, d.block_size, d.table_blocks, d.causal, d.window, d.max_new,
+                                        d.log_sum_exp, 0, d.q_stride, d.out_stride, d.block_stride, d.head_stride, d.slot_stride, d.scale};
+  return create_attention(what, same, d.code, partial_bytes, out);
+}
+
+fs_status fs_plan_create_cache_store8(const fs_cache8_desc* desc, fs_plan** out) { return create_cache8("fs_plan_create_cache_store8", desc, true, out); }
+fs_status fs_plan_create_cache_read8(const fs_cache8_desc* desc, fs_plan** out) { return create_cache8("fs_plan_create_cache_read8", desc, false, out); }
 
 }  // extern "C"
 
@@ -285,6 +375,8 @@ int fs::paged_launch(const PagedPlan& p, const void* const* in, void* const* out
   switch (p.kind) {
     case FS_SCHED_BLOCK_TABLES: return block_tables_launch(p.tables, in, out, stream, err);
     case FS_SCHED_ROTARY: return rotary_launch(p.rotary, in, out, stream, err);
+    case FS_SCHED_CACHE_STORE8: return cache8_launch(p.cache8, true, in, out, stream, err);
+    case FS_SCHED_CACHE_READ8: return cache8_launch(p.cache8, false, in, out, stream, err);
     default: return paged_attn_launch(p.attn, in, out, stream, err);
   }
 }

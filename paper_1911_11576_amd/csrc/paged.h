@@ -25,8 +25,16 @@ struct RotarySpec {
   bool one = false;                // a vector of a head to a thread
   int most_angles = 0;             // several heads to a thread: angles of a workgroup's rows
 };
+struct Cache8Spec {
+  fs_cache8_desc d{};
+  CacheLayout cache;               // of codes
+  int waves = 1;                   // store: wavefronts to a block's part of a request and head
+  int groups = 1, grid = 1;        // store: workgroups of a place; read: rows of a workgroup
+  int64_t items = 0;
+};
 struct PagedAttnSpec {
   fs_paged_attention_desc d{};
+  int code = -1;                   // fs_code of a cache in 8 bits; -1: it holds numbers of the type
   CacheLayout cache;
   int share = 1;                   // query heads to a key head
   // requests of up to few_rows rows: tiles of 16 * row_tiles, units of unit_keys keys, 1 << log_groups workgroups
@@ -44,11 +52,15 @@ struct PagedPlan {
   BlockTablesSpec tables;
   RotarySpec rotary;
   PagedAttnSpec attn;
+  Cache8Spec cache8;
 };
 
 int block_tables_launch(const BlockTablesSpec&, const void* const* in, void* const* out, void* stream, std::string* err);
 void rotary_geometry(RotarySpec*);
 int rotary_launch(const RotarySpec&, const void* const* in, void* const* out, void* stream, std::string* err);
+
+void cache8_geometry(Cache8Spec*, bool store);
+int cache8_launch(const Cache8Spec&, bool store, const void* const* in, void* const* out, void* stream, std::string* err);
 
 // Kernels, geometry and partial results of an attention plan; false: FS_ERR_UNSUPPORTED with *err.
 bool paged_attn_plan(PagedAttnSpec*, int* n_kernels, int64_t* lds_bytes, std::string* err);

@@ -1,0 +1,336 @@
+// Attention over a paged cache in 8 bits, few rows a request: bound by the reading of codes, half as many bytes as 16-bit keys and values have.
+//
+// The work is cut and joined as for a cache in 16 bits (FewLine, few_finish, paged_few_join); a wavefront takes 64 keys of a step, as many bytes as 32
+// there.  Codes come into LDS by direct loads of whole rows, scales with them, a key's to a lane; they become numbers of the storage type on their way from
+// LDS to the matrix unit: keys' codes as they stand, exactly, and the scores get the scales; for values in bf16 the weights get them, in fp16, where these
+// could leave the type's range, the numbers (powers of two exactly, of e4m3 the rest of a scale goes to the weights).
+#pragma once
+#include "cache8.h"
+#include "paged_few_impl.h"
+
+namespace fs {
+
+// 64 rows of D codes in LDS, 16 bytes x of row r in place x ^ f(r): eight lanes that read the same 16 bytes of eight rows of keys, and the eight rows of
+// a transposing read of values, 4g .. 4g + 3 and those 16 behind them, fall on different banks.
+template <int D> __device__ __forceinline__ int few8_turn_k(int row) { return D == 128 ? row & 7 : D == 64 ? row >> 1 & 3 : row >> 2 & 1; }
+template <int D> __device__ __forceinline__ int few8_turn_v(int row) { return D == 128 ? (row & 3) | (row >> 2 & 4) : D == 64 ? (row >> 1 & 1) | (row >> 3 & 2) : row >> 4 & 1; }
+
+template <int D, int NT, int W> struct Few8Lds {
+  FewLds<D, NT, W> few;            // (rows: 64 of D codes instead of 32 of D numbers)
+  float scales[W][2][2][64];       // by turns: of the keys, of the values
+};
+
+// Workgroup p of 1 << log_groups (of as many as there are places for tiles where log_groups is -1).
+template <typename T, class Code, int D, int NT, int W> __device__ __forceinline__ void paged8_few(const PagedArgs& a, Few8Lds<D, NT, W>& lds, int p) {
+  constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 64 * W, C = D / 16, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 64 rows
+  constexpr bool kWeights = __is_same(T, bf16_t);                         // the scales of values go to the weights, else into the numbers ...
+  constexpr bool kRest = !kWeights && __is_same(Code, E4m3);              // ... but for what is left of them beside a power of two
+  typedef Numbers<Code, T> Num;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int c = lane & 15, g = lane >> 4;
+  uint8_t *ksh = reinterpret_cast<uint8_t*>(lds.few.rows[w][0]), *vsh = reinterpret_cast<uint8_t*>(lds.few.rows[w][1]);
+  const uint32_t k_lds = lds_address(ksh), v_lds = lds_address(vsh), b_lds = lds_address(&lds.few.blocks[w][0][0]), s_lds = lds_address(&lds.scales[w][0][0][0]);
+  auto& blocks = lds.few.blocks;
+
+  FewLine<NT> line(a);
+  uint32_t u0 = 0, u1 = 1;
+  int head_in = 0;      // of its set
+  if (a.log_groups >= 0) {
+    if (a.neighbours) p = (p & 7) << (a.log_groups - 3) | p >> 3;      // (an XCD has every eighth workgroup)
+    head_in = p & ((1 << a.log_heads) - 1);
+    line.count();
+    const int log_groups = line.groups(), run = p >> a.log_heads;
+    if (run >> log_groups) return;
+    u0 = line.cut(run, log_groups); u1 = line.cut(run + 1, log_groups);
+  }
+  const uint8_t *kbase = static_cast<const uint8_t*>(a.k), *vbase = static_cast<const uint8_t*>(a.v);
+  const int in_block = (1 << a.cache.shift) - 1;
+
+  for (uint32_t cur = u0; cur < u1;) {
+    auto tile = a.log_groups < 0 ? line.whole(p) : line.find(cur);
+    if (!tile.there) break;
+    tile.head = tile.head << a.log_heads | head_in;
+    const int n = min(tile.n_units - tile.unit, (int)(u1 - cur));
+    const PagedRequest r = tile.r;
+    const int rows = r.fresh * a.share;
+    const int* table = a.tables + (int64_t)tile.b * a.width;
+    const int64_t head_at = (int64_t)tile.head * a.cache.head;
+    // ---- the rows: their queries as B operands, and the keys they see.  Two dots of 32 share 16 bytes of a key's row, so their k runs over d = 64 j + 16 g
+    // + 0 .. 7 and + 8 .. 15; of 32 that are left as usual.
+    u32x4 qf[NT][KS];
+    int until[NT], from[NT];
+    int most = 0, least = 0x7fffffff;      // over the tile's rows, uniform: no row sees keys from `most` on, every one sees those before `least` ...
+    int latest = 0;                        // ... and from `latest` on
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      const int row = tile.row0 + 16 * nt + c, there = min(row, rows - 1), token = there / a.share;
+      const uint16_t* q = static_cast<const uint16_t*>(a.q) + (r.first + token) * a.q_stride + (int64_t)(tile.head * a.share + there - token * a.share) * D;
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) qf[nt][ks] = *reinterpret_cast<const u32x4*>(q + (ks < KS / 2 * 2 ? 32 * (ks & ~1) + 16 * g + 8 * (ks & 1) : 32 * ks + 8 * g));
+      const int position = r.keys - r.fresh + token;
+      until[nt] = a.causal ? min(r.keys, position + 1) : r.keys;
+      from[nt] = a.window ? position + 1 - a.window : 0;
+    }
+    {
+      const int t0 = tile.row0 / a.share, t1 = (min(tile.row0 + M, rows) - 1) / a.share, back = r.keys - r.fresh + 1;
+      most = a.causal ? min(r.keys, back + t1) : r.keys;
+      least = a.causal ? min(r.keys, back + t0) : r.keys;
+      latest = a.window ? back + t1 - a.window : 0;
+    }
+    f32x4 o[NT][DT];
+    float m[NT], l[NT];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      m[nt] = -INFINITY; l[nt] = 0.f;
+#pragma unroll
+      for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
+    const int key_first = paged_first_key(a, r) + tile.unit * a.unit_keys;
+    const int key_end = min(most, key_first + n * a.unit_keys);
+    // ---- 64 keys: lane k's key has its row at `at`, its scales at `scale_at`; load i brings piece (64 i + lane) % C of key (64 i + lane) / C
+    int block;
+    bool ok;
+    int64_t at, scale_at;
+    auto block_of = [&](int key0) __attribute__((always_inline)) { return table + (min(key0 + lane, r.keys - 1) >> a.cache.shift); };
+    auto locate = [&](int key0) __attribute__((always_inline)) {
+      const int key = key0 + lane;
+      ok = key < key_end && (unsigned)block < (unsigned)a.cache.blocks;
+      at = head_at + (int64_t)(ok ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot;
+      scale_at = (int64_t)(ok ? block : 0) * a.kv_heads + tile.head;
+    };
+    auto row_of = [&](int i) { return (64 * i + lane) / C; };
+    auto bring_scales = [&](int turn) __attribute__((always_inline)) {
+      load_lds4(reinterpret_cast<const int*>(a.k_scales) + scale_at, s_lds + 512 * turn);
+      load_lds4(reinterpret_cast<const int*>(a.v_scales) + scale_at, s_lds + 512 * turn + 256);
+    };
+    auto bring_k = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = row_of(i), piece = (64 * i + lane) % C ^ few8_turn_k<D>(row);
+        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(kbase + __shfl((long long)at, row) + 16 * piece), k_lds + 1024 * i);
+      }
+    };
+    auto bring_v = [&]() __attribute__((always_inline)) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int row = row_of(i), piece = (64 * i + lane) % C ^ few8_turn_v<D>(row);
+        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(vbase + __shfl((long long)at, row) + 16 * piece), v_lds + 1024 * i);
+      }
+    };
+    const int kturn = few8_turn_k<D>(c), vrow = 4 * g + (c >> 1 & 3) + (c >> 3) * 16, vturn = few8_turn_v<D>(vrow);
+    const uint8_t *klane = ksh + c * D, *vlane = vsh + vrow * D + 8 * (c & 1);
+    auto work = [&](int key0, int turn) __attribute__((always_inline)) {
+      const uint64_t valid = __ballot(ok);                                            // of 64 keys those that are there
+      const bool plain = valid == ~0ull && key0 + 64 <= least && key0 >= latest;      // every row sees every one
+      const bool more = key0 + KEYS < key_end;
+      wait_loads<N>();      // the keys and the scales are there (the values may not be)
+      f32x4 s[NT][4];
+      float kscale[4], vscale[4];      // of keys 16 t + 4 g + 0 .. 3, which are of one block
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        kscale[t] = lds.scales[w][turn][0][16 * t + 4 * g] * a.scale2;
+        vscale[t] = lds.scales[w][turn][1][16 * t + 4 * g];
+      }
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) s[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < KS / 2; ++j) {
+          const u32x4 kc = *reinterpret_cast<const u32x4*>(klane + 16 * t * D + 16 * ((4 * j + g) ^ kturn));
+          const u32x4 k0 = Num::plain(u32x2{kc[0], kc[1]}), k1 = Num::plain(u32x2{kc[2], kc[3]});
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) {
+            s[nt][t] = Mfma<T>::run(k0, qf[nt][2 * j], s[nt][t]);
+            s[nt][t] = Mfma<T>::run(k1, qf[nt][2 * j + 1], s[nt][t]);
+          }
+        }
+        if constexpr (KS & 1) {
+          const u32x4 k0 = Num::plain(*reinterpret_cast<const u32x2*>(klane + 16 * t * D + 16 * ((4 * (KS / 2) + (g >> 1)) ^ kturn) + 8 * (g & 1)));
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) s[nt][t] = Mfma<T>::run(k0, qf[nt][KS - 1], s[nt][t]);
+        }
+      }
+      if (more) {
+        block = blocks[w][turn][lane];
+        locate(key0 + KEYS);
+        wait_lds_reads();
+        load_lds4(block_of(key0 + 2 * KEYS), b_lds + 256 * (turn ^ 1));
+        bring_scales(turn ^ 1);
+        bring_k();
+      }
+      u32x4 pb[NT][2];
+      uint32_t see[NT];      // of the lane's 16 scores those of keys that the row sees
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt) {
+        float top = m[nt];
+        see[nt] = 0;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = 16 * t + 4 * g + i;
+            float z = s[nt][t][i] * kscale[t];
+            if (!plain) {
+              const bool seen = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt];
+              see[nt] |= (uint32_t)seen << (4 * t + i);
+              z = seen ? z : -INFINITY;
+            }
+            s[nt][t][i] = z;
+            top = fmaxf(top, z);
+          }
+        top = rows_allreduce<MaxOp>(top);
+        const float low = top == -INFINITY ? 0.f : top;
+        const float keep = sum_factor(m[nt] - low);
+        m[nt] = top;
+        float sum = 0.f;
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s[nt][t][i] = __builtin_amdgcn_exp2f(s[nt][t][i] - low);
+            sum += s[nt][t][i];
+          }
+        l[nt] = l[nt] * keep + sum;
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) o[nt][dt][i] *= keep;
+        if constexpr (kWeights || kRest) {
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const float f = kRest ? rest_of(vscale[t]) : vscale[t];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][t][i] = plain || (see[nt] >> (4 * t + i) & 1) ? s[nt][t][i] * f : 0.f;      // (a key that is not seen may have any scale)
+          }
+        }
+        // rounded to T for the second dot alone: half a step of each weight, where fp32 weights would take that dot twice; the sum is of them unrounded
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+          pb[nt][u] = u32x4{Mfma<T>::pack(s[nt][2 * u][0], s[nt][2 * u][1]), Mfma<T>::pack(s[nt][2 * u][2], s[nt][2 * u][3]), Mfma<T>::pack(s[nt][2 * u + 1][0], s[nt][2 * u + 1][1]),
+                            Mfma<T>::pack(s[nt][2 * u + 1][2], s[nt][2 * u + 1][3])};
+      }
+      // what the numbers of values are multiplied by
+      float into[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) into[t] = kWeights ? 1.f : kRest ? power_of(vscale[t]) : vscale[t];
+      if (more) wait_loads<N + 3>();      // the values are there (the next keys may not be)
+      else wait_loads<0>();
+      if (!plain) {
+        // values of keys that are none do not count, whatever lies there; a NaN of another, or a number beyond the type's range, is added as it is in the
+        // rows that see it, and the second dot runs without it
+        auto odd = [&](float code, float scale) __attribute__((always_inline)) {
+          const float x = code * (kWeights ? 1.f : kRest ? power_of(scale) : scale);
+          return !(fabsf(x) < (kWeights ? INFINITY : 65520.f));
+        };
+        bool any = false;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          u32x4* v = reinterpret_cast<u32x4*>(vsh + 16 * (64 * i + lane));
+          const int row = row_of(i);
+          if (!(valid >> row & 1)) {
+            *v = u32x4{0u, 0u, 0u, 0u};
+          } else {
+            const float scale = lds.scales[w][turn][1][row];
+            if constexpr (__is_same(Code, E4m3)) {
+              const u32x4 x = *v;
+#pragma unroll
+              for (int j = 0; j < 4; ++j) any |= (((x[j] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) != 0;
+            }
+            if (!kWeights) any |= !(fabsf(kRest ? power_of(scale) : scale) * (__is_same(Code, E4m3) ? 448.f : 128.f) < 65520.f);
+          }
+        }
+        if (__ballot(any)) {
+          for (int k = 0; k < 64; ++k) {
+            const float scale = lds.scales[w][turn][1][k];
+#pragma unroll
+            for (int dt = 0; dt < DT; ++dt) {
+              float x[4];
+              Code::unpack(*reinterpret_cast<const uint32_t*>(vsh + k * D + 16 * (dt ^ few8_turn_v<D>(k)) + 4 * g), x);
+#pragma unroll
+              for (int nt = 0; nt < NT; ++nt) {
+                const bool seen = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                  const float y = x[i] * scale;
+                  o[nt][dt][i] += seen && odd(x[i], scale) ? (fabsf(y) < INFINITY ? copysignf(INFINITY, y) : y) : 0.f;
+                }
+              }
+            }
+          }
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            u32x4* v = reinterpret_cast<u32x4*>(vsh + 16 * (64 * i + lane));
+            const float scale = lds.scales[w][turn][1][row_of(i)];
+            u32x4 y = *v;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float x[4];
+              Code::unpack(y[j], x);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) y[j] = odd(x[e], scale) ? y[j] & ~(0xffu << (8 * e)) : y[j];
+            }
+            *v = y;
+          }
+        }
+        // a number's factor that is none would make NaN of a zero
+        if (!kWeights)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) into[t] = fabsf(into[t]) < INFINITY ? into[t] : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int dt = 0; dt < DT; ++dt) {
+          typedef int i32x2 __attribute__((ext_vector_type(2)));
+          typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
+          const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vlane + 32 * u * D + 16 * (dt ^ vturn))));
+          const u32x4 vt = kWeights ? Num::plain(vc) : Num::scaled(vc, into[2 * u], into[2 * u + 1]);
+#pragma unroll
+          for (int nt = 0; nt < NT; ++nt) o[nt][dt] = Mfma<T>::run(vt, pb[nt][u], o[nt][dt]);
+        }
+      if (more) {
+        wait_lds_reads();
+        bring_v();
+      }
+    };
+    // ---- the loop: this wavefront's 64 of every 64 W keys, the next ones' loads in flight
+    int key = key_first + 64 * w;
+    if (key < key_end) {
+      block = *block_of(key);
+      locate(key);
+      load_lds4(block_of(key + KEYS), b_lds);
+      bring_scales(0);
+      bring_k();
+      bring_v();
+      for (int turn = 0; key < key_end; key += KEYS, turn ^= 1) work(key, turn);
+    }
+    few_finish<T, D, NT, W>(a, lds.few, tile, n, 2 * p + (cur == u0 ? 0 : 1), o, m, l);
+    __syncthreads();      // (before the next tile's V)
+    cur += n;
+  }
+}
+
+template <typename T, class Code, int D, int NT, int W> __global__ __launch_bounds__(64 * W, 2) void paged8_few_kernel(const PagedArgs a) {
+  __shared__ __align__(1024) Few8Lds<D, NT, W> lds;
+  paged8_few<T, Code, D, NT, W>(a, lds, blockIdx.x);
+}
+
+template <typename T, class Code, int D, int NT> hipError_t paged8_few_launch(const PagedArgs& a, hipStream_t s) {
+  if (a.log_groups < 0 && a.few_grid > 256) hipLaunchKernelGGL((paged8_few_kernel<T, Code, D, NT, 4>), dim3(a.few_grid), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged8_few_kernel<T, Code, D, NT, 8>), dim3(a.few_grid), dim3(512), 0, s, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.log_groups < 0) return e;
+  return (__is_same(T, f16_t) ? paged_few_join_launch_f16 : paged_few_join_launch_bf16)(a, D, NT, s);
+}
+
+template <typename T, class Code> hipError_t paged8_few_launch_type(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) {
+  switch (dim) {
+    case 32: return row_tiles == 1 ? paged8_few_launch<T, Code, 32, 1>(a, s) : paged8_few_launch<T, Code, 32, 2>(a, s);
+    case 64: return row_tiles == 1 ? paged8_few_launch<T, Code, 64, 1>(a, s) : paged8_few_launch<T, Code, 64, 2>(a, s);
+    case 96: return row_tiles == 1 ? paged8_few_launch<T, Code, 96, 1>(a, s) : paged8_few_launch<T, Code, 96, 2>(a, s);
+    default: return row_tiles == 1 ? paged8_few_launch<T, Code, 128, 1>(a, s) : paged8_few_launch<T, Code, 128, 2>(a, s);
+  }
+}
+
+}  // namespace fs

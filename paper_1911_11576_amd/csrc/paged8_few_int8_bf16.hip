@@ -1,0 +1,6 @@
+// Attention over a paged cache in 8 bits, few rows a request: int8 codes, bf16.
+#include "paged8_few_impl.h"
+
+namespace fs {
+hipError_t paged8_few_launch_int8_bf16(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) { return paged8_few_launch_type<bf16_t, Int8>(a, dim, row_tiles, s); }
+}  // namespace fs

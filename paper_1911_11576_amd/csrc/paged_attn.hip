@@ -21,6 +21,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;      // at most
   const int64_t m = 16 * s->row_tiles;
   int64_t waves = many ? 4 : 8;      // of a workgroup
+  const int step = s->code < 0 ? 32 : 64, line = s->code < 0 ? 64 : 128;      // keys of a wavefront's step; elements of 128 bytes
   const bool any = d.tokens && d.requests;
   if (!many && keys <= 1024 && tiles <= 65536) {
     // No request is longer than four steps of 256 keys: a workgroup each tile, nothing to join (32 / 8 heads of 128: 8 requests of 100 keys 7.0 us, in
@@ -33,7 +34,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     // as many wavefronts as the chip holds, eight to a CU
     s->log_groups = many ? 9 : 8;
     s->few_grid = 1 << s->log_groups;
-    s->unit_keys = 32 * (int)waves;
+    s->unit_keys = step * (int)waves;
     // units are numbered in 31 bits
     while (tiles * (keys / s->unit_keys + 1) > 0x7fffffffll) {
       if (s->unit_keys >= (1 << 29)) { *err = "too many rows"; return false; }
@@ -44,27 +45,27 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     // Where heads lie side by side and share lines of 128 bytes: two (64 of 16000, 16 / 8 heads of 32: 209 us, 226 with eight, 323 without; 24 / 4 of
     // 96, 8000: 143 and 160).  Where they lie side by side in whole lines: none (256 of 4000, 32 / 8 of 128: 628 us, 676 with eight; 32 of 8000, 16 / 16 of 64: 170
     // and 195; one of 131072 alone gains, 97 -> 94).
-    const int most = s->cache.slot < s->cache.head ? 5 : s->cache.head % 64 ? 1 : 0;
+    const int most = s->cache.slot < s->cache.head ? 5 : s->cache.head % line ? 1 : 0;
     s->log_heads = std::min(most, __builtin_ctz((unsigned)d.kv_heads));
     s->neighbours = most > 0;
     if (any) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
   }
   s->partial_bytes = s->few_bytes;
   *n_kernels = s->log_groups < 0 ? 1 : 2;
-  *lds_bytes = std::max<int64_t>(waves * 128 * d.head_dim, waves * m * (d.head_dim + 4) * 4) + waves * (512 + 8 * m);
+  *lds_bytes = std::max<int64_t>(waves * 128 * d.head_dim, waves * m * (d.head_dim + 4) * 4) + waves * (512 + 8 * m + (s->code < 0 ? 0 : 1024));
   if (many) {
     s->slots = ((int64_t)d.tokens * s->share >> 7) + d.requests;
     if (s->slots * d.kv_heads > (1 << 24) - 2048) {      // (a grid has less than 2^32 threads)
       *err = "too many tiles for one grid"; return false; }
     if (any && d.requests <= kTileRequests) s->partial_bytes += 2ll * kTileShares * 128 * (d.head_dim + 2) * 4;
-    *lds_bytes = std::max<int64_t>(*lds_bytes, 512 * d.head_dim + 48);
+    *lds_bytes = std::max<int64_t>(*lds_bytes, 512 * d.head_dim + (s->code < 0 ? 48 : 1104));
   }
   return true;
 }
 
 std::string paged_attn_describe(const PagedAttnSpec& s) {
   char buf[320];
-  int n = snprintf(buf, sizeof buf, "paged_attention[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=%d%s", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.slots || (s.log_groups < 0 && s.few_grid > 256) ? 256 : 512,
+  int n = snprintf(buf, sizeof buf, "paged_attention%s[GRID,WARP,CTA] rows to a tile=%d, keys to a unit=%d; cta_num=%d, cta_size=%d%s", s.code < 0 ? "" : "8", 16 * s.row_tiles, s.unit_keys, s.few_grid, s.slots || (s.log_groups < 0 && s.few_grid > 256) ? 256 : 512,
                    s.log_groups < 0 ? "" : "; join[GRID,CTA]");
   if (s.slots) snprintf(buf + n, sizeof buf - n, "; requests of more than %d rows: rows to a tile=128, cta_num=%lld", s.few_rows, (long long)(s.slots * s.d.kv_heads));
   return buf;
@@ -74,6 +75,10 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   if (s.d.tokens == 0 || s.d.requests == 0) return 0;
   PagedArgs a{};
   a.q = in[0]; a.k = in[1]; a.v = in[2];
+  if (s.code >= 0) {
+    a.k_scales = static_cast<const float*>(in[3]); a.v_scales = static_cast<const float*>(in[4]);
+    in += 2;
+  }
   a.tables = static_cast<const int*>(in[3]); a.lengths = static_cast<const int*>(in[4]); a.starts = static_cast<const int*>(in[5]);
   a.out = out[0];
   if (s.d.log_sum_exp) a.lse = static_cast<float*>(out[1]);
@@ -91,10 +96,15 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.head_sets = s.d.kv_heads >> a.log_heads;
   if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;
   a.slots = (int)s.slots;
-  const bool f16 = s.d.dtype == FS_F16;
-  const hipError_t e = s.slots ? (f16 ? paged_mixed_launch_f16 : paged_mixed_launch_bf16)(a, s.d.head_dim, s.row_tiles, st)
-                               : (f16 ? paged_few_launch_f16 : paged_few_launch_bf16)(a, s.d.head_dim, s.row_tiles, st);
-  if (e != hipSuccess) { *err = std::string("paged_attention launch: ") + hipGetErrorString(e); return -1; }
+  const bool f16 = s.d.dtype == FS_F16, e4m3 = s.code == FS_CODE_E4M3;
+  hipError_t e;
+  if (s.code >= 0)
+    e = s.slots ? (e4m3 ? f16 ? paged8_mixed_launch_e4m3_f16 : paged8_mixed_launch_e4m3_bf16 : f16 ? paged8_mixed_launch_int8_f16 : paged8_mixed_launch_int8_bf16)(a, s.d.head_dim, s.row_tiles, st)
+                : (e4m3 ? f16 ? paged8_few_launch_e4m3_f16 : paged8_few_launch_e4m3_bf16 : f16 ? paged8_few_launch_int8_f16 : paged8_few_launch_int8_bf16)(a, s.d.head_dim, s.row_tiles, st);
+  else
+    e = s.slots ? (f16 ? paged_mixed_launch_f16 : paged_mixed_launch_bf16)(a, s.d.head_dim, s.row_tiles, st)
+                : (f16 ? paged_few_launch_f16 : paged_few_launch_bf16)(a, s.d.head_dim, s.row_tiles, st);
+  if (e != hipSuccess) { *err = std::string(s.code < 0 ? "paged_attention launch: " : "paged_attention8 launch: ") + hipGetErrorString(e); return -1; }
   return 0;
 }
 

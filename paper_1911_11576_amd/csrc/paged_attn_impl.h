@@ -27,6 +27,7 @@ struct PagedArgs {
   int few_rows;                    // requests of up to so many rows are the few-rows kernel's, the others the tile kernel's
   float* tile_partial;             // tiles of 128 rows: up to 2 * kTileShares of [128 * (D + 2)]
   int slots;                       // places for tiles in the order of the rows
+  const float *k_scales, *v_scales;      // a cache in 8 bits: [blocks, kv_heads]
 };
 
 // Workgroups of the tile kernel that the chip holds, two to a CU: what is shared out evenly.
@@ -140,8 +141,21 @@ __device__ __forceinline__ uint32_t lds_address(const void* p) { return (uint32_
 // few rows a request: the work split evenly over a fixed grid, then the parts joined
 hipError_t paged_few_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 hipError_t paged_few_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged_few_join_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged_few_join_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 // many rows a request, in tiles of 128, and few rows, in one
 hipError_t paged_mixed_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 hipError_t paged_mixed_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged_mixed_join_launch_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged_mixed_join_launch_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+// both over a cache in 8 bits; the joins are the same
+hipError_t paged8_few_launch_e4m3_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_few_launch_e4m3_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_few_launch_int8_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_few_launch_int8_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_mixed_launch_e4m3_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_mixed_launch_e4m3_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_mixed_launch_int8_f16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
+hipError_t paged8_mixed_launch_int8_bf16(const PagedArgs&, int dim, int row_tiles, hipStream_t);
 
 }  // namespace fs

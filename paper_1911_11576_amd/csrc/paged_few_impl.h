@@ -141,18 +141,81 @@ template <int D, int NT, int W> struct FewLds {
   float ms[W][M], ls[W][M];
 };
 
+// The end of n units of a tile: the wavefronts' results together, stored where that is all of it, else as partial results in place `part_at`.
+template <typename T, int D, int NT, int W>
+__device__ __forceinline__ void few_finish(const PagedArgs& a, FewLds<D, NT, W>& lds, const typename FewLine<NT>::Tile& tile, int n, int part_at, f32x4 (&o)[NT][D / 16], float (&m)[NT],
+                                           float (&l)[NT]) {
+  constexpr int DT = D / 16, M = 16 * NT, OP = FewLds<D, NT, W>::OP;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+  const int c = lane & 15, g = lane >> 4;
+  const PagedRequest r = tile.r;
+  const int rows = r.fresh * a.share;
+  float* osh = &lds.results[0][0];
+  auto& ms = lds.ms;
+  auto& ls = lds.ls;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] = rows_allreduce<SumOp>(l[nt]);
+    if (g == 0) { ms[w][16 * nt + c] = m[nt]; ls[w][16 * nt + c] = l[nt]; }
+  }
+  __syncthreads();      // (also: every wavefront is through with its V)
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int row = 16 * nt + c;
+    float top = -INFINITY;
+#pragma unroll
+    for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
+    const float f = top == -INFINITY ? 0.f : sum_factor(m[nt] - top);
+#pragma unroll
+    for (int dt = 0; dt < DT; ++dt) {
+      f32x4 x = o[nt][dt];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] *= f;
+      *reinterpret_cast<f32x4*>(osh + (w * M + row) * OP + 16 * dt + 4 * g) = x;
+    }
+  }
+  __syncthreads();
+  const bool whole = n == tile.n_units;
+  float* part = whole ? nullptr : a.partial + (int64_t)part_at * FewPart<D, NT>::kFloats;
+  for (int e = threadIdx.x; e < M * (D / 8); e += 64 * W) {
+    const int row = e / (D / 8), d = e % (D / 8) * 8;
+    float top = -INFINITY, sum = 0.f, x[8];
+#pragma unroll
+    for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
+    const float low = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < W; ++k) {
+      sum += ls[k][row] * __builtin_amdgcn_exp2f(ms[k][row] - low);
+      const f32x4 y0 = *reinterpret_cast<const f32x4*>(osh + (k * M + row) * OP + d), y1 = *reinterpret_cast<const f32x4*>(osh + (k * M + row) * OP + d + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) { x[i] += y0[i]; x[4 + i] += y1[i]; }
+    }
+    if (!whole) {
+      *reinterpret_cast<f32x4*>(part + row * D + d) = f32x4{x[0], x[1], x[2], x[3]};
+      *reinterpret_cast<f32x4*>(part + row * D + d + 4) = f32x4{x[4], x[5], x[6], x[7]};
+      if (d == 0) { part[M * D + row] = top; part[M * D + M + row] = sum; }
+    } else if (tile.row0 + row < rows) {
+      const int token = (tile.row0 + row) / a.share, head = tile.head * a.share + (tile.row0 + row) - token * a.share;
+      const float inv = sum == 0.f ? 0.f : 1.f / sum;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] *= inv;
+      *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) + (int64_t)(r.first + token) * a.out_stride + (int64_t)head * D + d) =
+          u32x4{Mfma<T>::pack(x[0], x[1]), Mfma<T>::pack(x[2], x[3]), Mfma<T>::pack(x[4], x[5]), Mfma<T>::pack(x[6], x[7])};
+      if (a.lse && d == 0) a.lse[(int64_t)(r.first + token) * a.q_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    }
+  }
+}
+
 // Workgroup p of 1 << log_groups (of as many as there are places for tiles where log_groups is -1).
 template <typename T, int D, int NT, int W> __device__ __forceinline__ void paged_few(const PagedArgs& a, FewLds<D, NT, W>& lds, int p) {
   constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 32 * W, C = D / 8, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 32 rows
-  constexpr int OP = FewLds<D, NT, W>::OP;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int c = lane & 15, g = lane >> 4;
   uint16_t *ksh = lds.rows[w][0], *vsh = lds.rows[w][1];
   const uint32_t k_lds = lds_address(ksh), v_lds = lds_address(vsh), b_lds = lds_address(&lds.blocks[w][0][0]);
-  float* osh = &lds.results[0][0];
   auto& blocks = lds.blocks;
-  auto& ms = lds.ms;
-  auto& ls = lds.ls;
 
   FewLine<NT> line(a);
   uint32_t u0 = 0, u1 = 1;
@@ -343,60 +406,7 @@ template <typename T, int D, int NT, int W> __device__ __forceinline__ void page
       bring(vbase, v_lds);
       for (int turn = 0; key < key_end; key += KEYS, turn ^= 1) work(key, turn);
     }
-    // ---- the wavefronts' results together
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      l[nt] = rows_allreduce<SumOp>(l[nt]);
-      if (g == 0) { ms[w][16 * nt + c] = m[nt]; ls[w][16 * nt + c] = l[nt]; }
-    }
-    __syncthreads();      // (also: every wavefront is through with its V)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = 16 * nt + c;
-      float top = -INFINITY;
-#pragma unroll
-      for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
-      const float f = top == -INFINITY ? 0.f : sum_factor(m[nt] - top);
-#pragma unroll
-      for (int dt = 0; dt < DT; ++dt) {
-        f32x4 x = o[nt][dt];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] *= f;
-        *reinterpret_cast<f32x4*>(osh + (w * M + row) * OP + 16 * dt + 4 * g) = x;
-      }
-    }
-    __syncthreads();
-    const bool whole = n == tile.n_units;
-    float* part = whole ? nullptr : a.partial + (int64_t)(2 * p + (cur == u0 ? 0 : 1)) * FewPart<D, NT>::kFloats;
-    for (int e = threadIdx.x; e < M * (D / 8); e += 64 * W) {
-      const int row = e / (D / 8), d = e % (D / 8) * 8;
-      float top = -INFINITY, sum = 0.f, x[8];
-#pragma unroll
-      for (int k = 0; k < W; ++k) top = fmaxf(top, ms[k][row]);
-      const float low = top == -INFINITY ? 0.f : top;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) x[i] = 0.f;
-#pragma unroll
-      for (int k = 0; k < W; ++k) {
-        sum += ls[k][row] * __builtin_amdgcn_exp2f(ms[k][row] - low);
-        const f32x4 y0 = *reinterpret_cast<const f32x4*>(osh + (k * M + row) * OP + d), y1 = *reinterpret_cast<const f32x4*>(osh + (k * M + row) * OP + d + 4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { x[i] += y0[i]; x[4 + i] += y1[i]; }
-      }
-      if (!whole) {
-        *reinterpret_cast<f32x4*>(part + row * D + d) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4*>(part + row * D + d + 4) = f32x4{x[4], x[5], x[6], x[7]};
-        if (d == 0) { part[M * D + row] = top; part[M * D + M + row] = sum; }
-      } else if (tile.row0 + row < rows) {
-        const int token = (tile.row0 + row) / a.share, head = tile.head * a.share + (tile.row0 + row) - token * a.share;
-        const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] *= inv;
-        *reinterpret_cast<u32x4*>(static_cast<uint16_t*>(a.out) + (int64_t)(r.first + token) * a.out_stride + (int64_t)head * D + d) =
-            u32x4{Mfma<T>::pack(x[0], x[1]), Mfma<T>::pack(x[2], x[3]), Mfma<T>::pack(x[4], x[5]), Mfma<T>::pack(x[6], x[7])};
-        if (a.lse && d == 0) a.lse[(int64_t)(r.first + token) * a.q_heads + head] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
-      }
-    }
+    few_finish<T, D, NT, W>(a, lds, tile, n, 2 * p + (cur == u0 ? 0 : 1), o, m, l);
     __syncthreads();      // (before the next tile's V)
     cur += n;
   }
@@ -493,6 +503,11 @@ template <typename T, int D, int NT> __global__ __launch_bounds__((FewJoin<D, NT
   paged_few_join<T, D, NT>(a, line, line.groups(), blockIdx.x);
 }
 
+template <typename T, int D, int NT> hipError_t paged_few_join_launch(const PagedArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3(a.few_grid - (1 << a.log_heads)), dim3(FewJoin<D, NT>::kThreads), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs& a, hipStream_t s) {
   // eight wavefronts fill a CU; whole tiles for more than every CU are done by four each, whose first loads pass while others work (D 128,
   // 32 / 8 heads: 32 requests of 500 keys 13.5 and 14.0 us, 64 27.3 and 23.8, 256 117 and 89; D 64, 256 of 100 50 and 21)
@@ -500,8 +515,16 @@ template <typename T, int D, int NT> hipError_t paged_few_launch(const PagedArgs
   else hipLaunchKernelGGL((paged_few_kernel<T, D, NT, 8>), dim3(a.few_grid), dim3(512), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.log_groups < 0) return e;
-  hipLaunchKernelGGL((paged_few_join_kernel<T, D, NT>), dim3(a.few_grid - (1 << a.log_heads)), dim3(FewJoin<D, NT>::kThreads), 0, s, a);
-  return hipGetLastError();
+  return paged_few_join_launch<T, D, NT>(a, s);
+}
+
+template <typename T> hipError_t paged_few_join_launch_type(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) {
+  switch (dim) {
+    case 32: return row_tiles == 1 ? paged_few_join_launch<T, 32, 1>(a, s) : paged_few_join_launch<T, 32, 2>(a, s);
+    case 64: return row_tiles == 1 ? paged_few_join_launch<T, 64, 1>(a, s) : paged_few_join_launch<T, 64, 2>(a, s);
+    case 96: return row_tiles == 1 ? paged_few_join_launch<T, 96, 1>(a, s) : paged_few_join_launch<T, 96, 2>(a, s);
+    default: return row_tiles == 1 ? paged_few_join_launch<T, 128, 1>(a, s) : paged_few_join_launch<T, 128, 2>(a, s);
+  }
 }
 
 template <typename T> hipError_t paged_few_launch_type(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) {
