@@ -6,14 +6,28 @@
 
 namespace fs {
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
 struct E4m3 {
   // The largest number of T that a code stands for, the scale being the one that a block with T's largest numbers gets: beyond, rounding could end at infinity.
   template <typename T> static constexpr float kMost = __is_same(T, f16_t) ? 61440.f : 0x1.ep+127f;
   // the least power of two that reaches x with a code of 448 = 1.75 * 2^8; 0 and subnormal numbers: one of -126 and less
   static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 135 + ((as_u32(x) & 0x7fffffu) > 0x600000u); }
-  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) {
-    const int lo = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
-    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, lo, true);
+  // the codes of four numbers over 2^power (pack), of four of T as they lie in memory (pack_words): rounded once, to the nearest and the even one of two
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d, int power) {
+    const float s = __builtin_ldexpf(1.f, power);
+    const s16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(s16x2{0, 0}, a, b, s, false);
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(lo, c, d, s, true));
+  }
+  template <typename T> static __device__ __forceinline__ uint32_t pack_words(uint32_t a, uint32_t b, int power) {
+    const float s = __builtin_ldexpf(1.f, power);
+    if constexpr (__is_same(T, bf16_t)) {
+      const s16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(s16x2{0, 0}, __builtin_bit_cast(bf16x2, a), s, false);
+      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(lo, __builtin_bit_cast(bf16x2, b), s, true));
+    } else {
+      const s16x2 lo = __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(s16x2{0, 0}, __builtin_bit_cast(f16x2, a), s, false);
+      return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_fp8_f16(lo, __builtin_bit_cast(f16x2, b), s, true));
+    }
   }
   static __device__ __forceinline__ void unpack(uint32_t c, float (&x)[4]) {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
@@ -26,9 +40,14 @@ struct Int8 {
   // 127 = 1.984375 * 2^6
   static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 133 + ((as_u32(x) & 0x7fffffu) > 0x7e0000u); }
   // 1.5 * 2^23 more leaves the nearest whole number, the even one of two, in the number's last bits
-  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d) {
-    const uint32_t w0 = as_u32(a + 0x1.8p23f), w1 = as_u32(b + 0x1.8p23f), w2 = as_u32(c + 0x1.8p23f), w3 = as_u32(d + 0x1.8p23f);
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d, int power) {
+    const float s = __builtin_ldexpf(1.f, -power);
+    const uint32_t w0 = as_u32(fmaf(a, s, 0x1.8p23f)), w1 = as_u32(fmaf(b, s, 0x1.8p23f)), w2 = as_u32(fmaf(c, s, 0x1.8p23f)), w3 = as_u32(fmaf(d, s, 0x1.8p23f));
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w3, w2, 0x0c0c0400u), __builtin_amdgcn_perm(w1, w0, 0x0c0c0400u), 0x05040100u);
+  }
+  template <typename T> static __device__ __forceinline__ uint32_t pack_words(uint32_t a, uint32_t b, int power) {
+    if constexpr (__is_same(T, bf16_t)) return pack(bf16_to_f32(a & 0xffffu), as_f32(a & 0xffff0000u), bf16_to_f32(b & 0xffffu), as_f32(b & 0xffff0000u), power);
+    else return pack(f16_to_f32(a & 0xffffu), f16_to_f32(a >> 16), f16_to_f32(b & 0xffffu), f16_to_f32(b >> 16), power);
   }
   static __device__ __forceinline__ void unpack(uint32_t c, float (&x)[4]) {
 #pragma unroll
@@ -48,6 +67,11 @@ __device__ __forceinline__ float rest_of(float s) {
   return e == 0 || e == 0x7f800000u ? s : as_f32((as_u32(s) & 0x807fffffu) | 0x3f800000u);
 }
 
+template <typename T> __device__ __forceinline__ uint32_t pack2(float a, float b) {
+  if constexpr (__is_same(T, bf16_t)) return pack2_bf16(a, b);
+  else return pack2_f16(a, b);
+}
+
 template <class Code, typename T> struct Numbers;
 template <typename T> struct Numbers<E4m3, T> {
   template <bool HI> static __device__ __forceinline__ uint32_t two(uint32_t c, float s) {
@@ -58,32 +82,52 @@ template <typename T> struct Numbers<E4m3, T> {
     return u32x4{two<false>(c[0], s0), two<true>(c[0], s0), two<false>(c[1], s1), two<true>(c[1], s1)};
   }
   static __device__ __forceinline__ u32x4 plain(u32x2 c) { return scaled(c, 1.f, 1.f); }
+  // all eight times one scale: one that takes() says, fast; or any, rounded to T
+  static __device__ __forceinline__ bool takes(float s) { return power_of(s) == s; }
+  static __device__ __forceinline__ u32x4 fast(u32x2 c, float s) { return scaled(c, s, s); }
+  static __device__ __forceinline__ u32x4 rounded(u32x2 c, float s) {
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      float x[4];
+      E4m3::unpack(c[i], x);
+      out[2 * i] = pack2<T>(x[0] * s, x[1] * s);
+      out[2 * i + 1] = pack2<T>(x[2] * s, x[3] * s);
+    }
+    return out;
+  }
 };
 template <typename T> struct Numbers<Int8, T> {
-  static __device__ __forceinline__ uint32_t two(float a, float b) {
-    if constexpr (__is_same(T, bf16_t)) return pack2_bf16(a, b);
-    else return pack2_f16(a, b);
-  }
   static __device__ __forceinline__ u32x4 scaled(u32x2 c, float s0, float s1) {
     float x[4], y[4];
     Int8::unpack(c[0], x);
     Int8::unpack(c[1], y);
-    return u32x4{two(x[0] * s0, x[1] * s0), two(x[2] * s0, x[3] * s0), two(y[0] * s1, y[1] * s1), two(y[2] * s1, y[3] * s1)};
+    return u32x4{pack2<T>(x[0] * s0, x[1] * s0), pack2<T>(x[2] * s0, x[3] * s0), pack2<T>(y[0] * s1, y[1] * s1), pack2<T>(y[2] * s1, y[3] * s1)};
   }
+  static __device__ __forceinline__ u32x4 rounded(u32x2 c, float s) { return scaled(c, s, s); }
   static __device__ __forceinline__ u32x4 plain(u32x2 c) {
     if constexpr (__is_same(T, bf16_t)) return scaled(c, 1.f, 1.f);
     else {
       // bytes without their sign, 128 more each, as the last bits of 1024 + them; less 1152
-      typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-      const h2 off = {(_Float16)1152.f, (_Float16)1152.f};
+      const f16x2 off = {(_Float16)1152.f, (_Float16)1152.f};
       u32x4 out;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const uint32_t w = __builtin_amdgcn_perm(0x64646464u, c[i / 2] ^ 0x80808080u, i & 1 ? 0x04030402u : 0x04010400u);
-        out[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, w) - off);
+        out[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, w) - off);
       }
       return out;
     }
+  }
+  // powers of two that fp16 holds, in its own products
+  static __device__ __forceinline__ bool takes(float s) { return __is_same(T, f16_t) && power_of(s) == s && s >= 0x1p-24f && s <= 0x1p15f; }
+  static __device__ __forceinline__ u32x4 fast(u32x2 c, float s) {
+    const u32x4 x = plain(c);
+    const f16x2 f = {(_Float16)s, (_Float16)s};
+    u32x4 out;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, (uint32_t)x[i]) * f);
+    return out;
   }
 };
 

@@ -184,6 +184,7 @@ fs_status create_cache8(const char* what, const fs_cache8_desc* desc, bool store
     *status = FS_ERR_UNSUPPORTED;
     if (dim % 16 || dim > 512) { *err = "head_dim must be a multiple of 16 up to 512"; return false; }
     if (d.k_stride * e % 16 || d.v_stride * e % 16) { *err = "rows of k and v must lie on 16 bytes"; return false; }
+    if (d.k_stride > (1 << 22) || d.v_stride > (1 << 22)) { *err = "k_stride or v_stride beyond 2^22"; return false; }
     if (!codes_fit(s.cache, d.block_size, err)) return false;
     fs::cache8_geometry(&s, store);
     fs::PagedPlan& g = p->paged;

@@ -1,28 +1,31 @@
 // Attention over a paged cache in 8 bits, few rows a request: bound by the reading of codes, half as many bytes as 16-bit keys and values have.
 //
-// The work is cut and joined as for a cache in 16 bits (FewLine, few_finish, paged_few_join); a wavefront takes 64 keys of a step, as many bytes as 32
-// there.  Codes come into LDS by direct loads of whole rows, scales with them, a key's to a lane; they become numbers of the storage type on their way from
+// The work is cut and joined as for a cache in 16 bits (FewLine, few_finish, paged_few_join).  A wavefront has 64 keys in LDS, as many bytes as 32
+// there: KT of them are a step's, the others of the steps to come.  Codes come into LDS by direct loads of whole rows, scales with them, a key's to a lane; they become numbers of the storage type on their way from
 // LDS to the matrix unit: keys' codes as they stand, exactly, and the scores get the scales; for values in bf16 the weights get them, in fp16, where these
 // could leave the type's range, the numbers (powers of two exactly, of e4m3 the rest of a scale goes to the weights).
 #pragma once
+#include <type_traits>
+
 #include "cache8.h"
 #include "paged_few_impl.h"
 
 namespace fs {
 
-// 64 rows of D codes in LDS, 16 bytes x of row r in place x ^ f(r): eight lanes that read the same 16 bytes of eight rows of keys, and the eight rows of
+// Rows of D codes in LDS, 16 bytes x of row r in place x ^ f(r): eight lanes that read the same 16 bytes of eight rows of keys, and the eight rows of
 // a transposing read of values, 4g .. 4g + 3 and those 16 behind them, fall on different banks.
 template <int D> __device__ __forceinline__ int few8_turn_k(int row) { return D == 128 ? row & 7 : D == 64 ? row >> 1 & 3 : row >> 2 & 1; }
 template <int D> __device__ __forceinline__ int few8_turn_v(int row) { return D == 128 ? (row & 3) | (row >> 2 & 4) : D == 64 ? (row >> 1 & 1) | (row >> 3 & 2) : row >> 4 & 1; }
 
 template <int D, int NT, int W> struct Few8Lds {
   FewLds<D, NT, W> few;            // (rows: 64 of D codes instead of 32 of D numbers)
-  float scales[W][2][2][64];       // by turns: of the keys, of the values
+  float scales[W][2][2][64];       // by turns: KT of the keys, KT of the values
 };
 
 // Workgroup p of 1 << log_groups (of as many as there are places for tiles where log_groups is -1).
-template <typename T, class Code, int D, int NT, int W> __device__ __forceinline__ void paged8_few(const PagedArgs& a, Few8Lds<D, NT, W>& lds, int p) {
-  constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = 64 * W, C = D / 16, N = D / 16;      // C: 16-byte pieces of a row; N: direct loads of 64 rows
+template <typename T, class Code, int D, int NT, int W, int KT> __device__ __forceinline__ void paged8_few(const PagedArgs& a, Few8Lds<D, NT, W>& lds, int p) {
+  constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = KT * W, S = 64 / KT, TT = KT / 16, C = D / 16, N = KT * D / 1024;      // S: steps in LDS; C: 16-byte pieces of a row; N: direct loads of KT rows
+  constexpr int E = 1 + KT / 32;      // loads of blocks to come and of scales
   constexpr bool kWeights = __is_same(T, bf16_t);                         // the scales of values go to the weights, else into the numbers ...
   constexpr bool kRest = !kWeights && __is_same(Code, E4m3);              // ... but for what is left of them beside a power of two
   typedef Numbers<Code, T> Num;
@@ -87,57 +90,66 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
     }
     const int key_first = paged_first_key(a, r) + tile.unit * a.unit_keys;
     const int key_end = min(most, key_first + n * a.unit_keys);
-    // ---- 64 keys: lane k's key has its row at `at`, its scales at `scale_at`; load i brings piece (64 i + lane) % C of key (64 i + lane) / C
+    // ---- KT keys: lane k's key, k mod KT of them, has its row at `at`, its scales at `scale_at`; load i brings piece (64 i + lane) % C of key (64 i + lane) / C
     int block;
-    bool ok;
     int64_t at, scale_at;
-    auto block_of = [&](int key0) __attribute__((always_inline)) { return table + (min(key0 + lane, r.keys - 1) >> a.cache.shift); };
-    auto locate = [&](int key0) __attribute__((always_inline)) {
-      const int key = key0 + lane;
-      ok = key < key_end && (unsigned)block < (unsigned)a.cache.blocks;
+    auto block_of = [&](int key0) __attribute__((always_inline)) { return table + (min(key0 + (lane & (KT - 1)), r.keys - 1) >> a.cache.shift); };
+    auto locate = [&](int key0) __attribute__((always_inline)) {      // -> which of the keys are there
+      const int key = key0 + (lane & (KT - 1));
+      const bool ok = key < key_end && (unsigned)block < (unsigned)a.cache.blocks;
       at = head_at + (int64_t)(ok ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot;
       scale_at = (int64_t)(ok ? block : 0) * a.kv_heads + tile.head;
+      return __ballot(ok);
     };
     auto row_of = [&](int i) { return (64 * i + lane) / C; };
-    auto bring_scales = [&](int turn) __attribute__((always_inline)) {
-      load_lds4(reinterpret_cast<const int*>(a.k_scales) + scale_at, s_lds + 512 * turn);
-      load_lds4(reinterpret_cast<const int*>(a.v_scales) + scale_at, s_lds + 512 * turn + 256);
-    };
-    auto bring_k = [&]() __attribute__((always_inline)) {
+    // (turn: the place in LDS of a step)
+    auto bring_blocks = [&](int key0, int turn) __attribute__((always_inline)) { load_lds4(block_of(key0), b_lds + 256 * turn); };
+    auto bring_k = [&](int turn) __attribute__((always_inline)) {
+      if constexpr (KT == 64) {
+        load_lds4(reinterpret_cast<const int*>(a.k_scales) + scale_at, s_lds + 512 * turn);
+        load_lds4(reinterpret_cast<const int*>(a.v_scales) + scale_at, s_lds + 512 * turn + 256);
+      } else {
+        load_lds4(reinterpret_cast<const int*>(lane < 32 ? a.k_scales : a.v_scales) + scale_at, s_lds + 512 * turn);
+      }
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = row_of(i), piece = (64 * i + lane) % C ^ few8_turn_k<D>(row);
-        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(kbase + __shfl((long long)at, row) + 16 * piece), k_lds + 1024 * i);
+        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(kbase + __shfl((long long)at, row) + 16 * piece), k_lds + KT * D * turn + 1024 * i);
       }
     };
-    auto bring_v = [&]() __attribute__((always_inline)) {
+    auto bring_v = [&](int turn) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = row_of(i), piece = (64 * i + lane) % C ^ few8_turn_v<D>(row);
-        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(vbase + __shfl((long long)at, row) + 16 * piece), v_lds + 1024 * i);
+        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(vbase + __shfl((long long)at, row) + 16 * piece), v_lds + KT * D * turn + 1024 * i);
       }
     };
     const int kturn = few8_turn_k<D>(c), vrow = 4 * g + (c >> 1 & 3) + (c >> 3) * 16, vturn = few8_turn_v<D>(vrow);
     const uint8_t *klane = ksh + c * D, *vlane = vsh + vrow * D + 8 * (c & 1);
-    auto work = [&](int key0, int turn) __attribute__((always_inline)) {
-      const uint64_t valid = __ballot(ok);                                            // of 64 keys those that are there
-      const bool plain = valid == ~0ull && key0 + 64 <= least && key0 >= latest;      // every row sees every one
-      const bool more = key0 + KEYS < key_end;
-      wait_loads<N>();      // the keys and the scales are there (the values may not be)
-      f32x4 s[NT][4];
-      float kscale[4], vscale[4];      // of keys 16 t + 4 g + 0 .. 3, which are of one block
+    uint64_t valid = 0, valid_next = 0;      // of the step's keys those that are there; S 2: of the next step's
+    auto work = [&](int key0, auto at_turn) __attribute__((always_inline)) {
+      constexpr int turn = decltype(at_turn)::value, ROWS = KT * D * turn;
+      constexpr uint64_t kAll = KT == 64 ? ~0ull : 0xffffffffull;
+      const bool plain = (valid & kAll) == kAll && key0 + KT <= least && key0 >= latest;      // every row sees every one
+      const bool next = key0 + KEYS < key_end, more = key0 + S * KEYS < key_end;              // steps to come, and to be requested
+      const float *kscales = &lds.scales[w][turn][0][0], *vscales = kscales + KT;
+      // the keys and the scales are there (the values, and what was requested behind them, may not be)
+      if (S == 1 || !next) wait_loads<N>();
+      else wait_loads<3 * N + E>();
+      f32x4 s[NT][TT];
+      float kscale[TT], vscale[TT];      // of keys 16 t + 4 g + 0 .. 3, which are of one block
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
-        kscale[t] = lds.scales[w][turn][0][16 * t + 4 * g] * a.scale2;
-        vscale[t] = lds.scales[w][turn][1][16 * t + 4 * g];
+      for (int t = 0; t < TT; ++t) {
+        kscale[t] = kscales[16 * t + 4 * g] * a.scale2;
+        vscale[t] = vscales[16 * t + 4 * g];
       }
 #pragma unroll
-      for (int t = 0; t < 4; ++t) {
+      for (int t = 0; t < TT; ++t) {
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) s[nt][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KS / 2; ++j) {
-          const u32x4 kc = *reinterpret_cast<const u32x4*>(klane + 16 * t * D + 16 * ((4 * j + g) ^ kturn));
+          const u32x4 kc = *reinterpret_cast<const u32x4*>(klane + ROWS + 16 * t * D + 16 * ((4 * j + g) ^ kturn));
           const u32x4 k0 = Num::plain(u32x2{kc[0], kc[1]}), k1 = Num::plain(u32x2{kc[2], kc[3]});
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) {
@@ -146,27 +158,27 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
           }
         }
         if constexpr (KS & 1) {
-          const u32x4 k0 = Num::plain(*reinterpret_cast<const u32x2*>(klane + 16 * t * D + 16 * ((4 * (KS / 2) + (g >> 1)) ^ kturn) + 8 * (g & 1)));
+          const u32x4 k0 = Num::plain(*reinterpret_cast<const u32x2*>(klane + ROWS + 16 * t * D + 16 * ((4 * (KS / 2) + (g >> 1)) ^ kturn) + 8 * (g & 1)));
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) s[nt][t] = Mfma<T>::run(k0, qf[nt][KS - 1], s[nt][t]);
         }
       }
+      uint64_t valid_new = 0;
       if (more) {
         block = blocks[w][turn][lane];
-        locate(key0 + KEYS);
+        valid_new = locate(key0 + S * KEYS);
         wait_lds_reads();
-        load_lds4(block_of(key0 + 2 * KEYS), b_lds + 256 * (turn ^ 1));
-        bring_scales(turn ^ 1);
-        bring_k();
+        bring_blocks(key0 + 2 * S * KEYS, turn);
+        bring_k(turn);
       }
-      u32x4 pb[NT][2];
-      uint32_t see[NT];      // of the lane's 16 scores those of keys that the row sees
+      u32x4 pb[NT][TT / 2];
+      uint32_t see[NT];      // of the lane's scores those of keys that the row sees
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float top = m[nt];
         see[nt] = 0;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < TT; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int k = 16 * t + 4 * g + i;
@@ -185,7 +197,7 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
         m[nt] = top;
         float sum = 0.f;
 #pragma unroll
-        for (int t = 0; t < 4; ++t)
+        for (int t = 0; t < TT; ++t)
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             s[nt][t][i] = __builtin_amdgcn_exp2f(s[nt][t][i] - low);
@@ -198,7 +210,7 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
           for (int i = 0; i < 4; ++i) o[nt][dt][i] *= keep;
         if constexpr (kWeights || kRest) {
 #pragma unroll
-          for (int t = 0; t < 4; ++t) {
+          for (int t = 0; t < TT; ++t) {
             const float f = kRest ? rest_of(vscale[t]) : vscale[t];
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[nt][t][i] = plain || (see[nt] >> (4 * t + i) & 1) ? s[nt][t][i] * f : 0.f;      // (a key that is not seen may have any scale)
@@ -206,16 +218,23 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
         }
         // rounded to T for the second dot alone: half a step of each weight, where fp32 weights would take that dot twice; the sum is of them unrounded
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
+        for (int u = 0; u < TT / 2; ++u)
           pb[nt][u] = u32x4{Mfma<T>::pack(s[nt][2 * u][0], s[nt][2 * u][1]), Mfma<T>::pack(s[nt][2 * u][2], s[nt][2 * u][3]), Mfma<T>::pack(s[nt][2 * u + 1][0], s[nt][2 * u + 1][1]),
                             Mfma<T>::pack(s[nt][2 * u + 1][2], s[nt][2 * u + 1][3])};
       }
       // what the numbers of values are multiplied by
-      float into[4];
+      float into[TT];
 #pragma unroll
-      for (int t = 0; t < 4; ++t) into[t] = kWeights ? 1.f : kRest ? power_of(vscale[t]) : vscale[t];
-      if (more) wait_loads<N + 3>();      // the values are there (the next keys may not be)
-      else wait_loads<0>();
+      for (int t = 0; t < TT; ++t) into[t] = kWeights ? 1.f : kRest ? power_of(vscale[t]) : vscale[t];
+      // the values are there (what was requested behind them may not be)
+      if constexpr (S == 1) {
+        if (more) wait_loads<N + E>();
+        else wait_loads<0>();
+      } else {
+        if (more) wait_loads<3 * N + 2 * E>();
+        else if (next) wait_loads<2 * N + E>();
+        else wait_loads<0>();
+      }
       if (!plain) {
         // values of keys that are none do not count, whatever lies there; a NaN of another, or a number beyond the type's range, is added as it is in the
         // rows that see it, and the second dot runs without it
@@ -226,12 +245,12 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
         bool any = false;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          u32x4* v = reinterpret_cast<u32x4*>(vsh + 16 * (64 * i + lane));
+          u32x4* v = reinterpret_cast<u32x4*>(vsh + ROWS + 16 * (64 * i + lane));
           const int row = row_of(i);
           if (!(valid >> row & 1)) {
             *v = u32x4{0u, 0u, 0u, 0u};
           } else {
-            const float scale = lds.scales[w][turn][1][row];
+            const float scale = vscales[row];
             if constexpr (__is_same(Code, E4m3)) {
               const u32x4 x = *v;
 #pragma unroll
@@ -241,12 +260,13 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
           }
         }
         if (__ballot(any)) {
-          for (int k = 0; k < 64; ++k) {
-            const float scale = lds.scales[w][turn][1][k];
 #pragma unroll
-            for (int dt = 0; dt < DT; ++dt) {
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll 1
+            for (int k = 0; k < KT; ++k) {
+              const float scale = vscales[k];
               float x[4];
-              Code::unpack(*reinterpret_cast<const uint32_t*>(vsh + k * D + 16 * (dt ^ few8_turn_v<D>(k)) + 4 * g), x);
+              Code::unpack(*reinterpret_cast<const uint32_t*>(vsh + ROWS + k * D + 16 * (dt ^ few8_turn_v<D>(k)) + 4 * g), x);
 #pragma unroll
               for (int nt = 0; nt < NT; ++nt) {
                 const bool seen = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt];
@@ -257,11 +277,10 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
                 }
               }
             }
-          }
 #pragma unroll
           for (int i = 0; i < N; ++i) {
-            u32x4* v = reinterpret_cast<u32x4*>(vsh + 16 * (64 * i + lane));
-            const float scale = lds.scales[w][turn][1][row_of(i)];
+            u32x4* v = reinterpret_cast<u32x4*>(vsh + ROWS + 16 * (64 * i + lane));
+            const float scale = vscales[row_of(i)];
             u32x4 y = *v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -276,34 +295,60 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
         // a number's factor that is none would make NaN of a zero
         if (!kWeights)
 #pragma unroll
-          for (int t = 0; t < 4; ++t) into[t] = fabsf(into[t]) < INFINITY ? into[t] : 0.f;
+          for (int t = 0; t < TT; ++t) into[t] = fabsf(into[t]) < INFINITY ? into[t] : 0.f;
       }
 #pragma unroll
-      for (int u = 0; u < 2; ++u)
+      for (int u = 0; u < TT / 2; ++u)
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt) {
           typedef int i32x2 __attribute__((ext_vector_type(2)));
           typedef __attribute__((address_space(3))) i32x2 lds_i32x2;
-          const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vlane + 32 * u * D + 16 * (dt ^ vturn))));
+          const u32x2 vc = __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2*)(vlane + ROWS + 32 * u * D + 16 * (dt ^ vturn))));
           const u32x4 vt = kWeights ? Num::plain(vc) : Num::scaled(vc, into[2 * u], into[2 * u + 1]);
 #pragma unroll
           for (int nt = 0; nt < NT; ++nt) o[nt][dt] = Mfma<T>::run(vt, pb[nt][u], o[nt][dt]);
         }
       if (more) {
         wait_lds_reads();
-        bring_v();
+        bring_v(turn);
       }
+      valid = S == 1 ? valid_new : valid_next;
+      if (S > 1) valid_next = valid_new;
     };
-    // ---- the loop: this wavefront's 64 of every 64 W keys, the next ones' loads in flight
-    int key = key_first + 64 * w;
+    // ---- the loop: this wavefront's KT of every KT W keys, what LDS has room for in flight
+    int key = key_first + KT * w;
     if (key < key_end) {
       block = *block_of(key);
-      locate(key);
-      load_lds4(block_of(key + KEYS), b_lds);
-      bring_scales(0);
-      bring_k();
-      bring_v();
-      for (int turn = 0; key < key_end; key += KEYS, turn ^= 1) work(key, turn);
+      const int block1 = S > 1 ? *block_of(key + KEYS) : 0;
+      valid = locate(key);
+      // The queries are there (as the block is, which was requested behind them): used here, or the compiler, which knows nothing of the loads into LDS, would wait
+      // for all loads where the loop uses them.
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int ks = 0; ks < KS; ++ks) asm volatile("" : "+v"(qf[nt][ks]));
+      bring_blocks(key + S * KEYS, 0);
+      bring_k(0);
+      bring_v(0);
+      if constexpr (S > 1) {
+        if (key + KEYS < key_end) {
+          block = block1;
+          valid_next = locate(key + KEYS);
+          bring_blocks(key + 3 * KEYS, 1);
+          bring_k(1);
+          bring_v(1);
+        }
+      }
+      for (;;) {
+        work(key, std::integral_constant<int, 0>{});
+        key += KEYS;
+        if (key >= key_end) break;
+        if constexpr (S > 1) {
+          work(key, std::integral_constant<int, 1>{});
+          key += KEYS;
+          if (key >= key_end) break;
+        }
+      }
     }
     few_finish<T, D, NT, W>(a, lds.few, tile, n, 2 * p + (cur == u0 ? 0 : 1), o, m, l);
     __syncthreads();      // (before the next tile's V)
@@ -311,9 +356,12 @@ template <typename T, class Code, int D, int NT, int W> __device__ __forceinline
   }
 }
 
+// Keys of a step: 64 at once cost fewer instructions for each; with two tiles of rows the registers hold the scores of 32 alone, and there is a step in flight
+// behind this one.
+constexpr int few8_keys(int nt) { return nt == 1 ? 64 : 32; }
 template <typename T, class Code, int D, int NT, int W> __global__ __launch_bounds__(64 * W, 2) void paged8_few_kernel(const PagedArgs a) {
   __shared__ __align__(1024) Few8Lds<D, NT, W> lds;
-  paged8_few<T, Code, D, NT, W>(a, lds, blockIdx.x);
+  paged8_few<T, Code, D, NT, W, few8_keys(NT)>(a, lds, blockIdx.x);
 }
 
 template <typename T, class Code, int D, int NT> hipError_t paged8_few_launch(const PagedArgs& a, hipStream_t s) {

@@ -1,15 +1,16 @@
-// Attention over a paged cache in 8 bits, many rows a request and few in one launch (paged_mixed_kernel, of codes).
+// Attention over a paged cache in 8 bits, many rows a request and few in one launch (paged_mixed_kernel, of codes).  Three workgroups to a CU up to head dim 64, where codes
+// on their way through registers leave no room for four (3 prompts of 2500, 16 heads of 64: 71 us, 78 with four and spilled registers).
 #pragma once
 #include "paged8_few_impl.h"
 #include "paged_tile_impl.h"
 
 namespace fs {
 
-template <typename T, class Code, int D, int NT> __global__ __launch_bounds__(256, (D <= 64 && NT == 1 ? 4 : 2)) void paged8_mixed_kernel(const PagedArgs a) {
-  __shared__ __align__(1024) union { Few8Lds<D, NT, 4> few; Tile8Shared<D> tile; } lds;
+template <typename T, class Code, int D, int NT> __global__ __launch_bounds__(256, (D <= 64 && NT == 1 ? 3 : 2)) void paged8_mixed_kernel(const PagedArgs a) {
+  __shared__ __align__(1024) union { Few8Lds<D, NT, 4> few; TileShared<D> tile; } lds;
   const int tiles = gridDim.x - a.few_grid, b = blockIdx.x;
   if (b < tiles) paged_tile<T, D, Code>(a, lds.tile, b);
-  else paged8_few<T, Code, D, NT, 4>(a, lds.few, b - tiles);
+  else paged8_few<T, Code, D, NT, 4, 32>(a, lds.few, b - tiles);
 }
 
 template <typename T, class Code, int D, int NT> hipError_t paged8_mixed_launch(const PagedArgs& a, hipStream_t s) {

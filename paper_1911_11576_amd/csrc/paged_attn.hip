@@ -21,7 +21,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;      // at most
   const int64_t m = 16 * s->row_tiles;
   int64_t waves = many ? 4 : 8;      // of a workgroup
-  const int step = s->code < 0 ? 32 : 64, line = s->code < 0 ? 64 : 128;      // keys of a wavefront's step; elements of 128 bytes
+  const int step = s->code < 0 ? 32 : 64, line = s->code < 0 ? 64 : 128;      // keys of a wavefront in LDS; elements of 128 bytes
   const bool any = d.tokens && d.requests;
   if (!many && keys <= 1024 && tiles <= 65536) {
     // No request is longer than four steps of 256 keys: a workgroup each tile, nothing to join (32 / 8 heads of 128: 8 requests of 100 keys 7.0 us, in
@@ -45,9 +45,12 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     // Where heads lie side by side and share lines of 128 bytes: two (64 of 16000, 16 / 8 heads of 32: 209 us, 226 with eight, 323 without; 24 / 4 of
     // 96, 8000: 143 and 160).  Where they lie side by side in whole lines: none (256 of 4000, 32 / 8 of 128: 628 us, 676 with eight; 32 of 8000, 16 / 16 of 64: 170
     // and 195; one of 131072 alone gains, 97 -> 94).
-    const int most = s->cache.slot < s->cache.head ? 5 : s->cache.head % line ? 1 : 0;
+    // Codes: neighbours with heads side by side too (one of 131072, 32 / 8 of 128: 59.3 us, 62.9 without), and sets of as many heads as share a line (80 of
+    // up to 30000, 64 / 16 heads of 32: sets of four 340 us, of two 416, of eight 347; of 64: two 422, four 429, none 595).
+    const bool side_by_side = s->cache.slot >= s->cache.head;
+    const int most = !side_by_side ? 5 : s->cache.head % line == 0 ? 0 : s->code >= 0 && s->cache.head <= 32 ? 2 : 1;
     s->log_heads = std::min(most, __builtin_ctz((unsigned)d.kv_heads));
-    s->neighbours = most > 0;
+    s->neighbours = most > 0 || s->code >= 0;
     if (any) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
   }
   s->partial_bytes = s->few_bytes;
@@ -58,7 +61,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     if (s->slots * d.kv_heads > (1 << 24) - 2048) {      // (a grid has less than 2^32 threads)
       *err = "too many tiles for one grid"; return false; }
     if (any && d.requests <= kTileRequests) s->partial_bytes += 2ll * kTileShares * 128 * (d.head_dim + 2) * 4;
-    *lds_bytes = std::max<int64_t>(*lds_bytes, 512 * d.head_dim + (s->code < 0 ? 48 : 1104));
+    *lds_bytes = std::max<int64_t>(*lds_bytes, 512 * d.head_dim + 48);
   }
   return true;
 }

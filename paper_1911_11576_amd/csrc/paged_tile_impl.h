@@ -213,21 +213,14 @@ template <int D> struct TileShared {
   TileLds<D> k[2], v[2];
   uint32_t flags[2][4], odds[4];                            // which of a wavefront's 16 keys are there; whether a value of them is infinite or NaN
 };
-// ... of a cache in 8 bits also whether a scale of theirs is no power of two, and then what is left of each beside one
-template <int D> struct Tile8Shared : TileShared<D> {
-  uint32_t uneven[2][4];
-  float k_rest[2][64], v_rest[2][64];
-};
 
 // A cache that holds numbers of the type itself, or one of the codes of 8 bits.
 struct NoCode {};
-template <class Code, int D> struct TileSharedOf { typedef Tile8Shared<D> type; };
-template <int D> struct TileSharedOf<NoCode, D> { typedef TileShared<D> type; };
 
-// Workgroup k of the tile kernel.  Codes come into registers, 16 of a lane at a time, and into LDS as numbers of T times their scales (powers of two: the codes'
-// own numbers, exactly; of e4m3 what is left of a scale is multiplied to scores and weights), so that each is made once for four wavefronts; from there on both kinds are the same.
-template <typename T, int D, class Code = NoCode> __device__ __forceinline__ void paged_tile(const PagedArgs& a, typename TileSharedOf<Code, D>::type& lds, int k) {
-  constexpr bool kCodes = !__is_same(Code, NoCode), kRest = __is_same(Code, E4m3);
+// Workgroup k of the tile kernel.  Codes come into registers, 16 of a lane at a time, and go into LDS as numbers of T times their scales (powers of two: exactly), so that
+// each is made once for four wavefronts; from there on both kinds are the same.
+template <typename T, int D, class Code = NoCode> __device__ __forceinline__ void paged_tile(const PagedArgs& a, TileShared<D>& lds, int k) {
+  constexpr bool kCodes = !__is_same(Code, NoCode);
   constexpr int KS = D / 16, DT = D / 32, CH = D / 32, K16 = 16 * D;
   auto &ksh = lds.k, &vsh = lds.v;
   auto& flags = lds.flags;
@@ -325,7 +318,7 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
   u32x4 kc[kCodes ? PL : 1], vc[kCodes ? PL : 1];
   float kscale = 0.f, vscale = 0.f;
   bool there_is = false;
-  auto fetch_codes = [&](int key0) __attribute__((always_inline)) {
+  auto fetch = [&](int key0) __attribute__((always_inline)) {
     const int key = key0 + skey;
     there_is = key < key_last && (unsigned)block < (unsigned)a.cache.blocks;
     const int64_t at = (int64_t)head * a.cache.head + (int64_t)(there_is ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot + 16 * (lane & 3);
@@ -340,19 +333,23 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
     kscale = a.k_scales[scale_at];
     vscale = a.v_scales[scale_at];
   };
-  auto put_codes = [&](int buf, auto code) __attribute__((always_inline)) {
+  auto put = [&](int buf, auto code) __attribute__((always_inline)) {
     typedef Numbers<decltype(code), T> Num;
-    const float ks = kRest ? power_of(kscale) : kscale, vs = kRest ? power_of(vscale) : vscale;
+    const bool even = __ballot(!Num::takes(kscale) || !Num::takes(vscale)) == 0;
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
       const int q = (lane & 3) + 4 * i;
       if (q >= P) continue;
       const int at = w * K16 + 512 * (q / 2) + srow * 32, x = 2 * (q & 1), turn = srow >> 2 & 3;
-      const u32x4 none = {0u, 0u, 0u, 0u};
-      *reinterpret_cast<u32x4*>(&ksh[buf].v[at + 8 * (x ^ turn)]) = Num::scaled(u32x2{kc[i][0], kc[i][1]}, ks, ks);
-      *reinterpret_cast<u32x4*>(&ksh[buf].v[at + 8 * ((x + 1) ^ turn)]) = Num::scaled(u32x2{kc[i][2], kc[i][3]}, ks, ks);
-      *reinterpret_cast<u32x4*>(&vsh[buf].v[at + 8 * (x ^ turn)]) = there_is ? Num::scaled(u32x2{vc[i][0], vc[i][1]}, vs, vs) : none;
-      *reinterpret_cast<u32x4*>(&vsh[buf].v[at + 8 * ((x + 1) ^ turn)]) = there_is ? Num::scaled(u32x2{vc[i][2], vc[i][3]}, vs, vs) : none;
+#pragma unroll
+      for (int v = 0; v < 2; ++v) {
+        const u32x4 c = v ? vc[i] : kc[i];
+        const float scale = v ? vscale : kscale;
+        const u32x2 c0 = {c[0], c[1]}, c1 = {c[2], c[3]};
+        uint16_t* rows = (v ? vsh[buf].v : ksh[buf].v) + at;
+        *reinterpret_cast<u32x4*>(rows + 8 * (x ^ turn)) = even ? Num::fast(c0, scale) : Num::rounded(c0, scale);
+        *reinterpret_cast<u32x4*>(rows + 8 * ((x + 1) ^ turn)) = even ? Num::fast(c1, scale) : Num::rounded(c1, scale);
+      }
     }
     const uint64_t good = __ballot(there_is);
     uint32_t flag = 0xffffu;
@@ -361,12 +358,6 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
       for (int k = 0; k < 16; ++k) flag |= (uint32_t)(good >> (4 * k) & 1) << k;
     }
     if (lane == 0) flags[buf][w] = flag;
-    if constexpr (kRest) {
-      const float kr = there_is ? rest_of(kscale) : 1.f, vr = there_is ? rest_of(vscale) : 1.f;
-      const bool uneven = __ballot(kr != 1.f || vr != 1.f) != 0;
-      if (lane == 0) lds.uneven[buf][w] = uneven;
-      if ((lane & 3) == 0) { lds.k_rest[buf][skey] = kr; lds.v_rest[buf][skey] = vr; }
-    }
   };
 
   auto compute = [&](int key0, int buf) __attribute__((always_inline)) {
@@ -423,15 +414,6 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
         s[t] = ks == 0 ? mfma32<T>(kf, qf[0], f32x16{}) : mfma32<T>(kf, qf[ks], s[t]);
       }
     // ---- softmax: the lane holds keys 32t + 8(i/4) + 4h + i%4 of its row
-    bool uneven = false;
-    if constexpr (kRest) {
-      uneven = __builtin_amdgcn_readfirstlane(lds.uneven[buf][0] | lds.uneven[buf][1] | lds.uneven[buf][2] | lds.uneven[buf][3]) != 0;
-      if (uneven)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[t][i] *= lds.k_rest[buf][32 * t + 8 * (i / 4) + 4 * h + i % 4];
-    }
     if (!plain) {
       // a bit for every key that the row sees, from the lane's first on
       auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };
@@ -471,17 +453,6 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
         sum += e;
       }
     l += sum;
-    if constexpr (kRest) {
-      if (uneven)
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) {
-            const int k = 32 * t + 8 * (i / 4) + 4 * h + i % 4;
-            const bool seen = ((t ? valid1 : valid0) >> (k & 31) & 1) && key0 + k < until && key0 + k >= from;
-            s[t][i] = seen ? s[t][i] * lds.v_rest[buf][k] : 0.f;
-          }
-    }
     u32x4 pb[4];      // rounded to T for the second dot alone: half a step of each weight; their sum is of them unrounded
 #pragma unroll
     for (int k = 0; k < 4; ++k)
@@ -509,18 +480,18 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
   if (steps > 0) {
     request_block(key_first);
     if constexpr (kCodes) {
-      fetch_codes(key_first);
+      fetch(key_first);
       request_block(key_first + 64);
-      put_codes(0, Code{});
+      put(0, Code{});
       __syncthreads();
       for (int i = 0; i < steps; ++i) {
         const int key0 = key_first + 64 * i;
         if (i + 1 < steps) {
-          fetch_codes(key0 + 64);
+          fetch(key0 + 64);
           request_block(key0 + 128);
         }
         compute(key0, i & 1);
-        if (i + 1 < steps) put_codes((i + 1) & 1, Code{});
+        if (i + 1 < steps) put((i + 1) & 1, Code{});
         __syncthreads();
       }
     } else {
