@@ -88,8 +88,8 @@ template <typename T, class Code, int D, int NT, int W, int KT> __device__ __for
 #pragma unroll
       for (int dt = 0; dt < DT; ++dt) o[nt][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
-    const int key_first = paged_first_key(a, r) + tile.unit * a.unit_keys;
-    const int key_end = min(most, key_first + n * a.unit_keys);
+    const int key_first = paged_first_key(a, r) + max(0, tile.unit - a.tile_units) * a.unit_keys;
+    const int key_end = min(most, paged_first_key(a, r) + (tile.unit + n - a.tile_units) * a.unit_keys);
     // ---- KT keys: lane k's key, k mod KT of them, has its row at `at`, its scales at `scale_at`; load i brings piece (64 i + lane) % C of key (64 i + lane) / C
     int block;
     int64_t at, scale_at;

@@ -21,7 +21,7 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
   const int64_t tiles = ((int64_t)d.tokens * s->share / (16 * s->row_tiles) + d.requests) * d.kv_heads;      // at most
   const int64_t m = 16 * s->row_tiles;
   int64_t waves = many ? 4 : 8;      // of a workgroup
-  const int step = s->code < 0 ? 32 : 64, line = s->code < 0 ? 64 : 128;      // keys of a wavefront in LDS; elements of 128 bytes
+  const int line = s->code < 0 ? 64 : 128;      // elements of 128 bytes
   const bool any = d.tokens && d.requests;
   if (!many && keys <= 1024 && tiles <= 65536) {
     // No request is longer than four steps of 256 keys: a workgroup each tile, nothing to join (32 / 8 heads of 128: 8 requests of 100 keys 7.0 us, in
@@ -34,9 +34,12 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     // as many wavefronts as the chip holds, eight to a CU
     s->log_groups = many ? 9 : 8;
     s->few_grid = 1 << s->log_groups;
-    s->unit_keys = step * (int)waves;
+    s->unit_keys = 32 * (int)waves;
+    // Of codes a tile's start and end take as long as half a step: it counts as a unit more (80 requests of up to 3000 keys, 32 / 8 heads of 128: 50.2 us, 54.5 without
+    // and in units of a whole step; 41 of up to 4 tokens behind 12000 in a window, 24 / 4 of 96: 43.6 and 45.6, 47.4 in these units without; two more 45.4).
+    s->tile_units = s->code < 0 ? 0 : 1;
     // units are numbered in 31 bits
-    while (tiles * (keys / s->unit_keys + 1) > 0x7fffffffll) {
+    while (tiles * (keys / s->unit_keys + 1 + s->tile_units) > 0x7fffffffll) {
       if (s->unit_keys >= (1 << 29)) { *err = "too many rows"; return false; }
       s->unit_keys *= 2;
     }
@@ -95,6 +98,7 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.unit_keys = s.unit_keys; a.log_groups = s.log_groups; a.few_grid = s.few_grid;
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.few_rows = s.few_rows;
+  a.tile_units = s.tile_units;
   a.log_heads = s.log_heads; a.neighbours = s.neighbours;
   a.head_sets = s.d.kv_heads >> a.log_heads;
   if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;

@@ -31,7 +31,7 @@ template <int NT> struct FewLine {
 
   __device__ __forceinline__ FewLine(const PagedArgs& args) : a(args) {}
   __device__ __forceinline__ int key_units(const PagedRequest& r) const {
-    return max(1, (r.keys - paged_first_key(a, r) + a.unit_keys - 1) / a.unit_keys);
+    return max(1, (r.keys - paged_first_key(a, r) + a.unit_keys - 1) / a.unit_keys) + a.tile_units;
   }
   __device__ __forceinline__ uint32_t units_of(const PagedRequest& r) const {
     if (r.fresh * a.share > a.few_rows) return 0;
