@@ -172,25 +172,34 @@ template <typename T, class Code, int D, int NT, int W, int KT> __device__ __for
         bring_k(turn);
       }
       u32x4 pb[NT][TT / 2];
-      uint32_t see[NT];      // of the lane's scores those of keys that the row sees
+      uint32_t see[NT][TT / 2];      // a bit for every key that the row sees, from the lane's first on
+      if (!plain) {
+        auto below = [](int n) { return n >= 32 ? 0xffffffffu : n <= 0 ? 0u : (1u << n) - 1; };
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+          for (int u = 0; u < TT / 2; ++u) {
+            const int first = key0 + 32 * u;
+            see[nt][u] = ((uint32_t)(valid >> 32 * u) & below(until[nt] - first) & ~below(from[nt] - first)) >> (4 * g);
+          }
+      }
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         float top = m[nt];
-        see[nt] = 0;
 #pragma unroll
         for (int t = 0; t < TT; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const int k = 16 * t + 4 * g + i;
-            float z = s[nt][t][i] * kscale[t];
-            if (!plain) {
-              const bool seen = (valid >> k & 1) && key0 + k < until[nt] && key0 + k >= from[nt];
-              see[nt] |= (uint32_t)seen << (4 * t + i);
-              z = seen ? z : -INFINITY;
-            }
-            s[nt][t][i] = z;
-            top = fmaxf(top, z);
-          }
+          for (int i = 0; i < 4; ++i) s[nt][t][i] *= kscale[t];
+        if (!plain) {
+#pragma unroll
+          for (int t = 0; t < TT; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[nt][t][i] = see[nt][t / 2] & 1u << (16 * (t & 1) + i) ? s[nt][t][i] : -INFINITY;
+        }
+#pragma unroll
+        for (int t = 0; t < TT; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = fmaxf(top, s[nt][t][i]);
         top = rows_allreduce<MaxOp>(top);
         const float low = top == -INFINITY ? 0.f : top;
         const float keep = sum_factor(m[nt] - low);
@@ -213,7 +222,13 @@ template <typename T, class Code, int D, int NT, int W, int KT> __device__ __for
           for (int t = 0; t < TT; ++t) {
             const float f = kRest ? rest_of(vscale[t]) : vscale[t];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][t][i] = plain || (see[nt] >> (4 * t + i) & 1) ? s[nt][t][i] * f : 0.f;      // (a key that is not seen may have any scale)
+            for (int i = 0; i < 4; ++i) s[nt][t][i] *= f;
+          }
+          if (!plain) {      // (a key that is not seen may have any scale)
+#pragma unroll
+            for (int t = 0; t < TT; ++t)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) s[nt][t][i] = see[nt][t / 2] & 1u << (16 * (t & 1) + i) ? s[nt][t][i] : 0.f;
           }
         }
         // rounded to T for the second dot alone: half a step of each weight, where fp32 weights would take that dot twice; the sum is of them unrounded
