@@ -186,17 +186,24 @@ template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_b
     // ---- codes from before
     if (lo && !nan && now != before) {
       const float ratio = __builtin_ldexpf(before, -power);
-      for (int r = r0; r < (r0 < rows ? lo : 0); r += rows) {
-        u32x2* c = reinterpret_cast<u32x2*>(codes + (int64_t)r * a.cache.slot + 8 * p);
-        const u32x2 was = *c;
-        u32x2 codes_now;
+      constexpr int U = 4;      // rows in flight
+      for (int r = r0; r < (r0 < rows ? lo : 0); r += U * rows) {
+        u32x2 was[U];
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          float z[4];
-          Code::unpack(was[i], z);
-          codes_now[i] = Code::pack(z[0] * ratio, z[1] * ratio, z[2] * ratio, z[3] * ratio, 0);
+        for (int u = 0; u < U; ++u)
+          if (r + u * rows < lo) was[u] = *reinterpret_cast<const u32x2*>(codes + (int64_t)(r + u * rows) * a.cache.slot + 8 * p);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (r + u * rows >= lo) continue;
+          u32x2 codes_now;
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            float z[4];
+            Code::unpack(was[u][i], z);
+            codes_now[i] = Code::pack(z[0] * ratio, z[1] * ratio, z[2] * ratio, z[3] * ratio, 0);
+          }
+          *reinterpret_cast<u32x2*>(codes + (int64_t)(r + u * rows) * a.cache.slot + 8 * p) = codes_now;
         }
-        *c = codes_now;
       }
     }
     // ---- the new ones
@@ -337,9 +344,12 @@ template <typename T, class Code> void read_launch(const Cache8Args& a, bool wid
 void cache8_geometry(Cache8Spec* s, bool store) {
   const fs_cache8_desc& d = s->d;
   if (store) {
+    // as many wavefronts and registers as a block's new tokens take, where the call's are shared evenly by its requests: eight pieces of a thread, or four (single
+    // tokens of 71 requests, 16 heads of 64, into blocks of 128: 4.4 us, 11.8 with what whole blocks take)
     const int rows = 64 / (d.head_dim / 8);      // of a wavefront at a time
-    s->waves = d.block_size > 8 * rows ? 4 : 1;
-    s->passes = d.block_size > 4 * rows ? 8 : 4;
+    const int64_t most = std::min<int64_t>(d.block_size, d.requests ? (d.tokens + d.requests - 1) / d.requests : 0);
+    s->waves = most > 8 * rows ? 4 : 1;
+    s->passes = most > 4 * rows ? 8 : 4;
     s->once = 2ll * d.tokens * d.kv_heads * d.head_dim * (d.dtype == FS_F32 ? 4 : 2) > (64ll << 20);
     s->places = (int)(((int64_t)d.tokens >> s->cache.shift) + 2ll * d.requests);
     s->groups = (2 * d.kv_heads * s->waves + 3) / 4;
