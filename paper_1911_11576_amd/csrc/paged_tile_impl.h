@@ -313,23 +313,23 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
     if (lane == 0) flags[buf][w] = flag;
   };
 
-  // ---- staging of codes: four lanes to a key, lane q of them pieces q and q + 4 of 16 codes
+  // ---- staging of codes: four lanes to a key, lane q of them pieces q and q + 4 of 16 codes (where there are no such, one that another lane has too)
   constexpr int P = D / 16, PL = (P + 3) / 4;
   u32x4 kc[kCodes ? PL : 1], vc[kCodes ? PL : 1];
   float kscale = 0.f, vscale = 0.f;
   bool there_is = false;
+  auto piece = [&](int i) { return (lane & (P - 4 * i >= 4 ? 3 : 1)) + 4 * i; };
   auto fetch = [&](int key0) __attribute__((always_inline)) {
     const int key = key0 + skey;
     there_is = key < key_last && (unsigned)block < (unsigned)a.cache.blocks;
-    const int64_t at = (int64_t)head * a.cache.head + (int64_t)(there_is ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot + 16 * (lane & 3);
+    const int64_t at = (int64_t)head * a.cache.head + (int64_t)(there_is ? block : 0) * a.cache.block + (int64_t)(key & in_block) * a.cache.slot;
     const int64_t scale_at = (int64_t)(there_is ? block : 0) * a.kv_heads + head;
     const uint8_t *k8 = static_cast<const uint8_t*>(a.k) + at, *v8 = static_cast<const uint8_t*>(a.v) + at;
 #pragma unroll
-    for (int i = 0; i < PL; ++i)
-      if ((lane & 3) + 4 * i < P) {
-        kc[i] = *reinterpret_cast<const u32x4*>(k8 + 64 * i);
-        vc[i] = *reinterpret_cast<const u32x4*>(v8 + 64 * i);
-      }
+    for (int i = 0; i < PL; ++i) {
+      kc[i] = *reinterpret_cast<const u32x4*>(k8 + 16 * piece(i));
+      vc[i] = *reinterpret_cast<const u32x4*>(v8 + 16 * piece(i));
+    }
     kscale = a.k_scales[scale_at];
     vscale = a.v_scales[scale_at];
   };
@@ -338,9 +338,7 @@ template <typename T, int D, class Code = NoCode> __device__ __forceinline__ voi
     const bool even = __ballot(!Num::takes(kscale) || !Num::takes(vscale)) == 0;
 #pragma unroll
     for (int i = 0; i < PL; ++i) {
-      const int q = (lane & 3) + 4 * i;
-      if (q >= P) continue;
-      const int at = w * K16 + 512 * (q / 2) + srow * 32, x = 2 * (q & 1), turn = srow >> 2 & 3;
+      const int q = piece(i), at = w * K16 + 512 * (q / 2) + srow * 32, x = 2 * (q & 1), turn = srow >> 2 & 3;
 #pragma unroll
       for (int v = 0; v < 2; ++v) {
         const u32x4 c = v ? vc[i] : kc[i];
