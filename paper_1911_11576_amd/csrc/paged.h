@@ -43,6 +43,7 @@ struct PagedAttnSpec {
   int log_heads = 0;               // key heads of a set, 1 << log_heads
   int tile_units = 0;              // units that a tile counts as beyond those of its keys
   bool neighbours = false;         // workgroups of an XCD have neighbouring runs
+  bool once = true;                // a cache in 8 bits: a head's codes share no lines with another's
   // the others: places for tiles of 128 rows (0: there are none)
   int64_t slots = 0, few_bytes = 0, partial_bytes = 0;
 };

@@ -23,7 +23,7 @@ template <int D, int NT, int W> struct Few8Lds {
 };
 
 // Workgroup p of 1 << log_groups (of as many as there are places for tiles where log_groups is -1).
-template <typename T, class Code, int D, int NT, int W, int KT> __device__ __forceinline__ void paged8_few(const PagedArgs& a, Few8Lds<D, NT, W>& lds, int p) {
+template <typename T, class Code, int D, int NT, int W, int KT, bool ONCE> __device__ __forceinline__ void paged8_few(const PagedArgs& a, Few8Lds<D, NT, W>& lds, int p) {
   constexpr int KS = D / 32, DT = D / 16, M = 16 * NT, KEYS = KT * W, S = 64 / KT, TT = KT / 16, C = D / 16, N = KT * D / 1024;      // S: steps in LDS; C: 16-byte pieces of a row; N: direct loads of KT rows
   constexpr int E = 1 + KT / 32;      // loads of blocks to come and of scales
   constexpr bool kWeights = __is_same(T, bf16_t);                         // the scales of values go to the weights, else into the numbers ...
@@ -114,14 +114,14 @@ template <typename T, class Code, int D, int NT, int W, int KT> __device__ __for
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = row_of(i), piece = (64 * i + lane) % C ^ few8_turn_k<D>(row);
-        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(kbase + __shfl((long long)at, row) + 16 * piece), k_lds + KT * D * turn + 1024 * i);
+        load_lds16<0, ONCE>(reinterpret_cast<const uint16_t*>(kbase + __shfl((long long)at, row) + 16 * piece), k_lds + KT * D * turn + 1024 * i);
       }
     };
     auto bring_v = [&](int turn) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < N; ++i) {
         const int row = row_of(i), piece = (64 * i + lane) % C ^ few8_turn_v<D>(row);
-        load_lds16<0, true>(reinterpret_cast<const uint16_t*>(vbase + __shfl((long long)at, row) + 16 * piece), v_lds + KT * D * turn + 1024 * i);
+        load_lds16<0, ONCE>(reinterpret_cast<const uint16_t*>(vbase + __shfl((long long)at, row) + 16 * piece), v_lds + KT * D * turn + 1024 * i);
       }
     };
     const int kturn = few8_turn_k<D>(c), vrow = 4 * g + (c >> 1 & 3) + (c >> 3) * 16, vturn = few8_turn_v<D>(vrow);
@@ -374,25 +374,30 @@ template <typename T, class Code, int D, int NT, int W, int KT> __device__ __for
 // Keys of a step: 64 at once cost fewer instructions for each; with two tiles of rows the registers hold the scores of 32 alone, and there is a step in flight
 // behind this one.
 constexpr int few8_keys(int nt) { return nt == 1 ? 64 : 32; }
-template <typename T, class Code, int D, int NT, int W> __global__ __launch_bounds__(64 * W, 2) void paged8_few_kernel(const PagedArgs a) {
+template <typename T, class Code, int D, int NT, int W, bool ONCE> __global__ __launch_bounds__(64 * W, 2) void paged8_few_kernel(const PagedArgs a) {
   __shared__ __align__(1024) Few8Lds<D, NT, W> lds;
-  paged8_few<T, Code, D, NT, W, few8_keys(NT)>(a, lds, blockIdx.x);
+  paged8_few<T, Code, D, NT, W, few8_keys(NT), ONCE>(a, lds, blockIdx.x);
 }
 
-template <typename T, class Code, int D, int NT> hipError_t paged8_few_launch(const PagedArgs& a, hipStream_t s) {
-  if (a.log_groups < 0 && a.few_grid > 256) hipLaunchKernelGGL((paged8_few_kernel<T, Code, D, NT, 4>), dim3(a.few_grid), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((paged8_few_kernel<T, Code, D, NT, 8>), dim3(a.few_grid), dim3(512), 0, s, a);
+// Codes go past the caches (ONCE) where no other head has codes in their lines (a.once); heads of 128 fill lines, and those of 32 gain nothing from it.  (80 requests of up
+// to 30000 keys, heads of 64, 16 of them: one behind the other 265 us, through the caches 294; side by side 420 and 363; 16 of 32 side by side 339 and 260.)
+template <typename T, class Code, int D, int NT, bool ONCE> hipError_t paged8_few_launch(const PagedArgs& a, hipStream_t s) {
+  if (a.log_groups < 0 && a.few_grid > 256) hipLaunchKernelGGL((paged8_few_kernel<T, Code, D, NT, 4, ONCE>), dim3(a.few_grid), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((paged8_few_kernel<T, Code, D, NT, 8, ONCE>), dim3(a.few_grid), dim3(512), 0, s, a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || a.log_groups < 0) return e;
   return (__is_same(T, f16_t) ? paged_few_join_launch_f16 : paged_few_join_launch_bf16)(a, D, NT, s);
 }
+template <typename T, class Code, int D, bool ONCE> hipError_t paged8_few_launch_rows(const PagedArgs& a, int row_tiles, hipStream_t s) {
+  return row_tiles == 1 ? paged8_few_launch<T, Code, D, 1, ONCE>(a, s) : paged8_few_launch<T, Code, D, 2, ONCE>(a, s);
+}
 
 template <typename T, class Code> hipError_t paged8_few_launch_type(const PagedArgs& a, int dim, int row_tiles, hipStream_t s) {
   switch (dim) {
-    case 32: return row_tiles == 1 ? paged8_few_launch<T, Code, 32, 1>(a, s) : paged8_few_launch<T, Code, 32, 2>(a, s);
-    case 64: return row_tiles == 1 ? paged8_few_launch<T, Code, 64, 1>(a, s) : paged8_few_launch<T, Code, 64, 2>(a, s);
-    case 96: return row_tiles == 1 ? paged8_few_launch<T, Code, 96, 1>(a, s) : paged8_few_launch<T, Code, 96, 2>(a, s);
-    default: return row_tiles == 1 ? paged8_few_launch<T, Code, 128, 1>(a, s) : paged8_few_launch<T, Code, 128, 2>(a, s);
+    case 32: return paged8_few_launch_rows<T, Code, 32, false>(a, row_tiles, s);
+    case 64: return a.once ? paged8_few_launch_rows<T, Code, 64, true>(a, row_tiles, s) : paged8_few_launch_rows<T, Code, 64, false>(a, row_tiles, s);
+    case 96: return a.once ? paged8_few_launch_rows<T, Code, 96, true>(a, row_tiles, s) : paged8_few_launch_rows<T, Code, 96, false>(a, row_tiles, s);
+    default: return paged8_few_launch_rows<T, Code, 128, true>(a, row_tiles, s);
   }
 }
 

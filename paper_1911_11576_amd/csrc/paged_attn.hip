@@ -48,14 +48,15 @@ bool paged_attn_plan(PagedAttnSpec* s, int* n_kernels, int64_t* lds_bytes, std::
     // Where heads lie side by side and share lines of 128 bytes: two (64 of 16000, 16 / 8 heads of 32: 209 us, 226 with eight, 323 without; 24 / 4 of
     // 96, 8000: 143 and 160).  Where they lie side by side in whole lines: none (256 of 4000, 32 / 8 of 128: 628 us, 676 with eight; 32 of 8000, 16 / 16 of 64: 170
     // and 195; one of 131072 alone gains, 97 -> 94).
-    // Codes: neighbours with heads side by side too (one of 131072, 32 / 8 of 128: 59.3 us, 62.9 without), and sets of as many heads as share a line (80 of
-    // up to 30000, 64 / 16 heads of 32: sets of four 340 us, of two 416, of eight 347; of 64: two 422, four 429, none 595).
+    // Codes: neighbours with heads side by side too (one of 131072, 32 / 8 of 128: 59.3 us, 62.9 without), and sets of the heads that share lines, of 64 two, else
+    // four (80 of up to 30000 keys, 16 heads of 32: sets of four 259 us, of eight 264; 8 of 96: 362, two 385; 16 of 64: two 363, four 364, eight 380).
     const bool side_by_side = s->cache.slot >= s->cache.head;
-    const int most = !side_by_side ? 5 : s->cache.head % line == 0 ? 0 : s->code >= 0 && s->cache.head <= 32 ? 2 : 1;
+    const int most = !side_by_side ? 5 : s->cache.head % line == 0 ? 0 : s->code >= 0 && s->cache.head != 64 ? 2 : 1;
     s->log_heads = std::min(most, __builtin_ctz((unsigned)d.kv_heads));
     s->neighbours = most > 0 || s->code >= 0;
     if (any) s->few_bytes = (2ll << s->log_groups) * m * (d.head_dim + 2) * 4;
   }
+  s->once = s->cache.slot < s->cache.head || s->cache.head % 128 == 0;
   s->partial_bytes = s->few_bytes;
   *n_kernels = s->log_groups < 0 ? 1 : 2;
   *lds_bytes = std::max<int64_t>(waves * 128 * d.head_dim, waves * m * (d.head_dim + 4) * 4) + waves * (512 + 8 * m + (s->code < 0 ? 0 : 1024));
@@ -98,7 +99,7 @@ int paged_attn_launch(const PagedAttnSpec& s, const void* const* in, void* const
   a.unit_keys = s.unit_keys; a.log_groups = s.log_groups; a.few_grid = s.few_grid;
   hipStream_t st = static_cast<hipStream_t>(stream);
   a.few_rows = s.few_rows;
-  a.tile_units = s.tile_units;
+  a.tile_units = s.tile_units; a.once = s.once;
   a.log_heads = s.log_heads; a.neighbours = s.neighbours;
   a.head_sets = s.d.kv_heads >> a.log_heads;
   if (s.partial_bytes) a.tile_partial = a.partial + s.few_bytes / 4;

@@ -28,6 +28,7 @@ struct PagedArgs {
   float* tile_partial;             // tiles of 128 rows: up to 2 * kTileShares of [128 * (D + 2)]
   int slots;                       // places for tiles in the order of the rows
   const float *k_scales, *v_scales;      // a cache in 8 bits: [blocks, kv_heads]
+  int once;                        // ... a head's codes share no lines of 128 bytes with another's
   int tile_units;                  // few rows: units that a tile counts as beyond those of its keys, before them
 };
 
