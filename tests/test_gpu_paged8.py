@@ -185,6 +185,37 @@ def test_store_of_many_requests(requests, heads):
     check_store("bf16", "e4m3", x, tables, codes, scales, lengths, np.concatenate([[0], np.cumsum(new)]), 8)
 
 
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dim, size", [(128, 64), (64, 256), (512, 8), (80, 128)])
+def test_store_of_a_long_request_among_single_tokens(code, dim, size):
+    """What registers hold goes by the requests' mean share; the long one's blocks have more, and begin behind many tokens from before."""
+    rng, g = np.random.default_rng(dim), torch.Generator("cuda").manual_seed(dim)
+    new = np.array([1] * 30 + [2 * size + 77] + [1] * 30)
+    lengths = new + rng.integers(0, 3 * size, len(new))
+    lengths[30] = new[30] + size - 5
+    tables, codes, scales = cache_of(rng, code, lengths, 2, dim, size)
+    x = [numbers_of(g, "bf16", int(new.sum()), 2, dim) for _ in range(2)]
+    x[0][5:9] *= 64      # (their blocks grow)
+    check_store("bf16", code, x, tables, codes, scales, lengths, np.concatenate([[0], np.cumsum(new)]), size, order=("head", "token")[size % 3 == 1])
+
+
+def test_store_past_the_caches():
+    """More than 64 MiB of keys and values: they are read past the caches."""
+    new, heads, dim, size = [9000, 7900, 500], 16, 64, 64
+    g = torch.Generator("cuda").manual_seed(8)
+    lengths = np.array(new) + [0, 1000, 70]
+    tables, codes, scales = cache_of(np.random.default_rng(8), "int8", [0, 1000, 70], heads, dim, size, extra=300)
+    free = np.setdiff1d(np.arange(len(codes[0])), tables)
+    wide, at = np.full((3, 200), -1), 0
+    for b, n in enumerate(lengths):
+        held, need = -(-[0, 1000, 70][b] // size), -(-n // size)
+        wide[b, :held] = tables[b, :held]
+        wide[b, held:need] = free[at:at + need - held]
+        at += need - held
+    x = [numbers_of(g, "f16", sum(new), heads, dim) for _ in range(2)]
+    check_store("f16", "int8", x, wide, codes, scales, lengths, np.concatenate([[0], np.cumsum(new)]), size, order="token")
+
+
 # ---------------------------------------------------------------------------------------------------- read
 
 def run_read(dtype, code, t, tables, codes, scales, lengths, starts, size, order="head", pad=0):
@@ -373,6 +404,19 @@ def test_attention_of_chunks_among_many_requests(requests, chunks):
     new[rng.permutation(requests)[:chunks]] = rng.integers(20, 60, chunks)
     keys = new + rng.integers(0, 200, requests)
     check_attention(problem(2, "f16", "int8", keys.tolist(), new.tolist(), 8, 2, 32, 16))
+
+
+@pytest.mark.parametrize("table_keys, long", [(64, 60), (2048, 1900)])
+def test_attention_of_thousands_of_requests(table_keys, long):
+    """4200 requests, a few long ones behind the first 4096: whole tiles, and a line of units."""
+    rng = np.random.default_rng(table_keys)
+    keys = rng.integers(1, 40, 4200)
+    keys[[3, 4100, 4199]] = long
+    c = problem(13, "bf16", "e4m3", keys.tolist(), [1] * 4200, 4, 2, 32, 8)
+    wide = np.full((4200, table_keys // 8), -1)
+    wide[:, :c["tables"].shape[1]] = c["tables"][:, :wide.shape[1]]
+    c["tables"] = wide
+    check_attention(c, max_new=1)
 
 
 @pytest.mark.parametrize("order", ["head", "token"])
