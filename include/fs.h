@@ -532,7 +532,7 @@ typedef enum { FS_CODE_E4M3 = 0, FS_CODE_INT8 = 1 } fs_code;
  *   outputs   k_cache, v_cache, k_scales, v_scales (read and written)
  * Nothing is written for rows of no request or before a request's first token, for blocks outside [0, blocks), and in other places of a block than those of the request's tokens.  Two
  * requests that write to one block leave it undefined.
- * dtype FS_F32, FS_F16 or FS_BF16, head_dim a multiple of 16 up to 512, rows of k and v on 16 bytes.
+ * dtype FS_F32, FS_F16 or FS_BF16, head_dim a multiple of 16 up to 512, rows of k and v on 16 bytes, k_stride and v_stride up to 2^22, requests up to 65536, tokens up to 2^30.
  * Errors: FS_ERR_INVALID, FS_ERR_UNSUPPORTED (a head_dim, stride or block_size that no kernel takes), FS_ERR_NOMEM. */
 typedef struct {
   int32_t dtype, code;             /* of k and v; fs_code */
@@ -554,9 +554,9 @@ fs_status fs_plan_create_cache_read8(const fs_cache8_desc* desc, fs_plan** out);
 /* Attention of new tokens over the cache in 8 bits: fs_plan_create_paged_attention with the numbers that the codes stand for as keys and values.
  *   inputs    q, k_cache, v_cache, k_scales, v_scales, tables, lengths, starts
  *   outputs   out; with log_sum_exp also lse; with partial_bytes not 0 also the partial results
- * Any scales are taken: values (and where a request may have more than 32 rows, keys) whose scale is no power of two may be rounded to dtype, where 16-bit keys and values had been rounded
- * before; numbers beyond its range may count as infinities.  What is said there of masks, blocks outside, lengths, rows of no request and NaN holds here, for scales too: one of
- * a block that a row does not see never reaches it. block_size 8 to 1024, strides of the cache multiples of 16 codes. */
+ * Any scales are taken: where one is no power of two, the numbers of its block may be rounded to dtype, as keys and values held in dtype had been; numbers beyond the
+ * range of dtype may count as infinities.  What is said there of masks, blocks outside, lengths, rows of no request and NaN holds here, of scales too: one of
+ * a block that a row does not see never reaches it.  block_size 8 to 1024, strides of the cache multiples of 16 codes; limits and errors are the same. */
 typedef struct {
   int32_t dtype, code;             /* FS_F16 or FS_BF16: q, out; fs_code: the caches */
   int32_t requests, tokens, q_heads, kv_heads, head_dim;

@@ -3,7 +3,9 @@
 // The work is cut and joined as for a cache in 16 bits (FewLine, few_finish, paged_few_join).  A wavefront has 64 keys in LDS, as many bytes as 32
 // there: KT of them are a step's, the others of the steps to come.  Codes come into LDS by direct loads of whole rows, scales with them, a key's to a lane; they become numbers of the storage type on their way from
 // LDS to the matrix unit: keys' codes as they stand, exactly, and the scores get the scales; for values in bf16 the weights get them, in fp16, where these
-// could leave the type's range, the numbers (powers of two exactly, of e4m3 the rest of a scale goes to the weights).
+// could leave the type's range, the numbers (powers of two exactly, of e4m3 the rest of a scale goes to the weights).  6.2 TB/s for 80 requests of one token behind up to
+// 30000 keys (32 / 8 heads of 128, e4m3, 267 us; a copy of 1 GiB reaches 6.65), 4.5 for one behind 131072 (int8, 60 us, of which the reading takes 40: the start of table
+// and keys 4, wavefronts that end after others 7, results 1, the second kernel 6).
 #pragma once
 #include <type_traits>
 
