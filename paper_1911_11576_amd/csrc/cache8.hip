@@ -113,15 +113,16 @@ template <typename T> __device__ __forceinline__ uint32_t wave_top(uint32_t v) {
 
 // W wavefronts do a block's part of one request and one head of K or V: the new numbers, N pieces of 8 of a thread's in registers, their maximum, the
 // block's scale, its codes from before in that scale where it grew, the new codes.  What registers do not hold is read twice.  Bound by memory: 4.9 TB/s for 11014
-// tokens, 8 heads of 128 in bf16 (13.8 us; with 16 numbers of a thread side by side and conversions by single instructions in fp32 18.5), 4.7 for 21253 tokens, 16 heads
-// of 64 in fp16 side by side, into blocks of 64 (27.8 us; K and V by one wavefront 38, four wavefronts to a block 39).  ONCE: k and v past the caches where
-// both are more than 64 MiB (those 28 us, 33 through the caches; the first 17 and 14).
+// tokens, 8 heads of 128 in bf16 (13.8 us; with 16 numbers of a thread side by side and conversions by single instructions in fp32 18.5), 5.0 for 21253 tokens, 16 heads
+// of 64 in fp16 side by side, into blocks of 64 (26.1 us; K and V by one wavefront 38, four wavefronts to a block 39).  ONCE: k and v past the caches where
+// both are more than 64 MiB (those 26.1 us, 29.1 through the caches; the first 15.5 and 13.9).  The grid: all heads of a place one after the other on one XCD (workgroup n is
+// dispatched to XCD n mod 8), eight places side by side; the 26.1 us are 27.1 where a place's heads go round the XCDs, 28.0 where all places of four heads come first.
 template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_bounds__(256) void cache8_store_kernel(const Cache8Args a) {
   __shared__ uint32_t tops[4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
   const int size = 1 << a.cache.shift;
-  for (int at = blockIdx.x; at < a.places; at += gridDim.x)
-  for (int group = blockIdx.y; group < a.groups; group += gridDim.y) {
+  for (int at = 8 * blockIdx.y + (blockIdx.x & 7); at < a.places; at += 8 * gridDim.y)
+  for (int group = blockIdx.x >> 3; group < a.groups; group += gridDim.x >> 3) {
     // ---- where: request b's blocks begin at place start / size + 2 b, as many places as it can touch blocks
     const int unit = group * (4 / W) + wave / W;
     auto place = [&](int first, int b) { return (first >> a.cache.shift) + 2 * b; };
@@ -357,7 +358,8 @@ void cache8_geometry(Cache8Spec* s, bool store) {
     s->places = (int)(((int64_t)d.tokens >> s->cache.shift) + 2ll * d.requests);
     s->groups = (2 * d.kv_heads * s->waves + 3) / 4;
     s->grid_groups = std::min(s->groups, 1 << 10);
-    s->grid = (int)std::min<int64_t>(s->places, (1 << 23) / s->grid_groups);      // (a grid has less than 2^32 threads)
+    // (eight times as many rows of a grid have less than 2^32 threads)
+    s->grid = (int)std::min<int64_t>(((int64_t)s->places + 7) / 8, std::min(65535, (1 << 20) / s->grid_groups));
     return;
   }
   // two rows (or runs of rows side by side) to a wavefront where there are enough of them: each has four columns of both in flight
@@ -392,7 +394,7 @@ int cache8_launch(const Cache8Spec& s, bool store, const void* const* in, void* 
   hipStream_t st = static_cast<hipStream_t>(stream);
   const bool e4m3 = d.code == FS_CODE_E4M3;
   if (store) {
-    const dim3 grid(s.grid, s.grid_groups);
+    const dim3 grid(8 * s.grid_groups, s.grid);
     auto go = [&](auto type) {
       typedef decltype(type) T;
       if (s.once) e4m3 ? store_launch<T, E4m3, true>(a, s.passes, s.waves, grid, st) : store_launch<T, Int8, true>(a, s.passes, s.waves, grid, st);

@@ -29,7 +29,7 @@ struct Cache8Spec {
   fs_cache8_desc d{};
   CacheLayout cache;               // of codes
   int waves = 1, passes = 2;       // store: wavefronts to a block's part of a request and head, pieces that a thread holds
-  int groups = 1, grid = 1;        // store: workgroups of a place; read: rows of a workgroup
+  int groups = 1, grid = 1;        // store: workgroups of a place, eights of places in the grid; read: rows of a workgroup, workgroups
   bool once = false, wide = false; // store: k and v past the caches; read: a token has 64 times 8 codes and more
   int places = 0, grid_groups = 1; // store: of requests' blocks; workgroups of a place in the grid
 };

@@ -199,6 +199,18 @@ def test_store_of_a_long_request_among_single_tokens(code, dim, size):
     check_store("bf16", code, x, tables, codes, scales, lengths, np.concatenate([[0], np.cumsum(new)]), size, order=("head", "token")[size % 3 == 1])
 
 
+def test_store_of_more_than_a_grid():
+    """More heads and more places of requests' blocks than the grid has rows and columns: a workgroup takes several of both."""
+    requests, heads = 4200, 2080
+    rng, g = np.random.default_rng(9), torch.Generator("cuda").manual_seed(9)
+    new, lengths = np.zeros(requests, int), np.zeros(requests, int)
+    for b, n, m in [(0, 3, 11), (1, 1, 8), (700, 9, 9), (4090, 1, 2), (4097, 17, 30), (4199, 2, 9)]:
+        new[b], lengths[b] = n, m
+    tables, codes, scales = cache_of(rng, "e4m3", lengths, heads, 16, 8)
+    x = [numbers_of(g, "bf16", int(new.sum()), heads, 16) for _ in range(2)]
+    check_store("bf16", "e4m3", x, tables, codes, scales, lengths, np.concatenate([[0], np.cumsum(new)]), 8)
+
+
 def test_store_past_the_caches():
     """More than 64 MiB of keys and values: they are read past the caches."""
     new, heads, dim, size = [9000, 7900, 500], 16, 64, 64
