@@ -145,6 +145,9 @@ template <typename T, class Code, int D, int NT, int W, int KT, bool ONCE> __dev
         kscale[t] = kscales[16 * t + 4 * g] * a.scale2;
         vscale[t] = vscales[16 * t + 4 * g];
       }
+      // fp16, where a row may not see every key: also that of the values of key `lane`, since bring_k has the scales of a later step written to their place
+      float lane_scale = 1.f;
+      if (!kWeights && !plain) lane_scale = vscales[lane & (KT - 1)];
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
 #pragma unroll
@@ -264,10 +267,10 @@ template <typename T, class Code, int D, int NT, int W, int KT, bool ONCE> __dev
         for (int i = 0; i < N; ++i) {
           u32x4* v = reinterpret_cast<u32x4*>(vsh + ROWS + 16 * (64 * i + lane));
           const int row = row_of(i);
+          const float scale = kWeights ? 1.f : __shfl(lane_scale, row);
           if (!(valid >> row & 1)) {
             *v = u32x4{0u, 0u, 0u, 0u};
           } else {
-            const float scale = vscales[row];
             if constexpr (__is_same(Code, E4m3)) {
               const u32x4 x = *v;
 #pragma unroll
@@ -281,7 +284,7 @@ template <typename T, class Code, int D, int NT, int W, int KT, bool ONCE> __dev
           for (int dt = 0; dt < DT; ++dt)
 #pragma unroll 1
             for (int k = 0; k < KT; ++k) {
-              const float scale = vscales[k];
+              const float scale = kWeights ? 1.f : as_f32(__builtin_amdgcn_readlane(as_u32(lane_scale), k));
               float x[4];
               Code::unpack(*reinterpret_cast<const uint32_t*>(vsh + ROWS + k * D + 16 * (dt ^ few8_turn_v<D>(k)) + 4 * g), x);
 #pragma unroll
@@ -297,7 +300,7 @@ template <typename T, class Code, int D, int NT, int W, int KT, bool ONCE> __dev
 #pragma unroll
           for (int i = 0; i < N; ++i) {
             u32x4* v = reinterpret_cast<u32x4*>(vsh + ROWS + 16 * (64 * i + lane));
-            const float scale = vscales[row_of(i)];
+            const float scale = kWeights ? 1.f : __shfl(lane_scale, row_of(i));
             u32x4 y = *v;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {

@@ -1,0 +1,116 @@
+"""Attention over the paged cache in 8 bits where a step of the few-rows kernel whose keys not every row sees has another step behind it: in front of a window, and
+around blocks that are none.  The scales of the two steps must not be taken for each other's.  Tolerances as in test_gpu_paged8.py.
+
+A step is 32 or 64 keys of each of four or eight wavefronts, so a wavefront has a step behind a masked one in windows of 256 keys and more.
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import paged8
+from test_gpu_paged import f64
+from test_gpu_paged8 import CODES, buffers, check_attention, inputs, plan_of, problem
+
+pytestmark = pytest.mark.gpu
+
+SIZE = 16
+CASES = [   # window, new tokens, query heads, key heads, head dim, keys of the shortest request, requests, new tokens of one more request
+    (512, 1, 4, 2, 64, 700, 32, 0),        # whole tiles, eight wavefronts
+    (512, 3, 4, 2, 128, 700, 32, 0),
+    (256, 1, 4, 2, 64, 300, 160, 0),       # ... four
+    (256, 3, 4, 2, 32, 300, 160, 0),
+    (512, 1, 4, 2, 128, 1500, 32, 0),      # a line of units
+    (512, 3, 4, 2, 96, 1500, 32, 0),
+    (1000, 3, 16, 2, 64, 1500, 32, 0),     # two tiles of rows, two steps in LDS
+    (1000, 3, 16, 2, 96, 1500, 32, 0),
+    (256, 1, 4, 2, 64, 600, 32, 60),       # among chunks
+    (256, 3, 4, 2, 128, 600, 32, 60),
+    (512, 1, 20, 1, 64, 600, 32, 60),
+]
+
+EVERY = [("f16", c) for c in CASES] + [("bf16", c) for c in (CASES[0], CASES[3], CASES[7], CASES[8])]      # (bf16 takes the scales of values another way, into the weights)
+
+
+def windowed(case, dtype, code):
+    """Requests of every remainder by 32, and block 0 nobody's."""
+    window, new, q_heads, heads, dim, keys, requests, chunk = case
+    lengths, fresh = [keys + b for b in range(32)] * (requests // 32), [new] * requests
+    if chunk:
+        lengths, fresh = lengths + [keys + 77], fresh + [chunk]
+    c = problem(window + new, dtype, code, lengths, fresh, q_heads, heads, dim, SIZE, ("head", "token")[new == 3])
+    block_0_of_nobody(c)
+    return c, window, 0 if chunk else new
+
+
+def block_0_of_nobody(c):
+    spare = np.setdiff1d(np.arange(len(c["codes"][0])), c["tables"])[0]
+    for a in (*c["codes"], *c["scales"]):
+        a[[0, spare]] = a[[spare, 0]]
+    c["tables"][c["tables"] == 0] = spare
+
+
+@pytest.mark.parametrize("value", [float("nan"), 2.0**14])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype, case", EVERY, ids=str)
+def test_window_behind_which_block_0_is_nobodys(dtype, case, code, value):
+    """Lanes without a key have the scale of block 0."""
+    c, window, max_new = windowed(case, dtype, code)
+    for s in c["scales"]:
+        s[0] = value
+    check_attention(c, window, True, max_new)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype, case", EVERY, ids=str)
+def test_scale_that_is_none_in_a_windows_first_block(dtype, case, code, value):
+    """Values of the block with the first key that a request's last token sees, finite ones behind it: no result of the request is a number."""
+    c, window, max_new = windowed(case, dtype, code)
+    for b, n in enumerate(c["lengths"]):
+        c["scales"][1][c["tables"][b, (n - window) // SIZE]] = value
+    plan, nbytes = plan_of(c, window, True, max_new)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+        torch.cuda.synchronize()
+    got = f64(outs[0])
+    assert np.isnan(got).all() if np.isnan(value) else not np.isfinite(got).any()
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype, case", EVERY, ids=str)
+def test_large_scales_behind_a_windows_first_keys(dtype, case, code):
+    """Large codes of values under a small scale in the window's first half, small codes under a scale in the second half with which the large ones would leave
+    fp16's range."""
+    c, window, max_new = windowed(case, dtype, code)
+    rng = np.random.default_rng(1)
+    most, scale, small = (448, 2.0**8, 1) if code == "e4m3" else (127, 2.0**10, 8)
+    for b, n in enumerate(c["lengths"]):
+        for j in range(-(-int(n) // SIZE)):
+            page = c["tables"][b, j]
+            m = min(SIZE, int(n) - j * SIZE)
+            shape = c["codes"][1][page, :, :m].shape
+            behind = j * SIZE >= n - window // 2
+            x = rng.uniform(-small, small, shape) if behind else rng.uniform(0.6 * most, most, shape) * rng.choice([-1, 1], shape)
+            c["codes"][1][page, :, :m] = paged8.coded(x, code)
+            c["scales"][1][page] = scale if behind else 2.0**-6
+    check_attention(c, window, True, max_new)
+
+
+@pytest.mark.parametrize("value", [float("nan"), 2.0**14])
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("new, q_heads, heads, dim, keys, window, chunk", [
+    (1, 4, 2, 128, 3000, 0, 0), (3, 16, 2, 64, 3000, 0, 0), (2, 4, 2, 64, 900, 0, 0), (1, 4, 2, 96, 3000, 1000, 0), (1, 4, 2, 64, 900, 0, 50), (1, 20, 1, 32, 900, 0, 50)])
+def test_blocks_that_are_none_in_the_middle(new, q_heads, heads, dim, keys, window, chunk, dtype, code, value):
+    """A sixth of all blocks: their lanes have the scale of block 0."""
+    lengths, fresh = [keys, keys - 13, keys - 300, keys // 2], [new] * 4
+    if chunk:
+        lengths, fresh = lengths + [keys - 50], fresh + [chunk]
+    c = problem(keys + new, dtype, code, lengths, fresh, q_heads, heads, dim, SIZE)
+    block_0_of_nobody(c)
+    for s in c["scales"]:
+        s[0] = value
+    rng = np.random.default_rng(keys)
+    c["tables"] = np.where(rng.random(c["tables"].shape) < 1 / 6, rng.choice([-1, len(c["codes"][0]), 2**31 - 1], c["tables"].shape), c["tables"])
+    check_attention(c, window, True, 0 if chunk else new)
