@@ -56,13 +56,12 @@ def least_power(most, code):
     return max(-126, e)
 
 
-def cut(x, code, dtype):
-    """Numbers whose code would stand for an infinity of dtype, cut to the largest that does not: of the code below at the scale of dtype's largest."""
+def cut(x, code, dtype, scale):
+    """Numbers whose code over `scale` would stand for an infinity of dtype, cut to the largest that does not."""
     top = {"f16": 65504.0, "bf16": float(2.0**127 * (2 - 2.0**-7)), "f32": float(np.finfo(np.float32).max)}[dtype]
-    scale = math.ldexp(1.0, least_power(top, code))
     grid = _ORDER if code == "e4m3" else np.arange(128.0)
     limit = max(v * scale for v in grid if v * scale <= top)
-    return np.clip(x, -limit, limit)
+    return np.copysign(np.minimum(np.abs(x), limit), x)
 
 
 def store(x, codes, scales, tables, lengths, starts, code, dtype):
@@ -99,7 +98,7 @@ def store(x, codes, scales, tables, lengths, starts, code, dtype):
                 scale = math.ldexp(1.0, power)
                 if lo and scale != before:
                     codes[page, h, :lo] = coded(values(codes[page, h, :lo], code) * (before / scale), code)
-                codes[page, h, lo:hi] = coded(cut(here, code, dtype) / scale, code)
+                codes[page, h, lo:hi] = coded(cut(here, code, dtype, scale) / scale, code)
                 scales[page, h] = scale
     return codes, scales
 

@@ -8,9 +8,14 @@ namespace fs {
 
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
+template <typename T> constexpr float kLargest = __is_same(T, f16_t) ? 65504.f : __is_same(T, bf16_t) ? 0x1.fep+127f : 0x1.fffffep+127f;
+
 struct E4m3 {
-  // The largest number of T that a code stands for, the scale being the one that a block with T's largest numbers gets: beyond, rounding could end at infinity.
-  template <typename T> static constexpr float kMost = __is_same(T, f16_t) ? 61440.f : 0x1.ep+127f;
+  // The largest number that a code over 2^power stands for and that is one of T: beyond, rounding could end at infinity.
+  template <typename T> static __device__ __forceinline__ float most(int power) {
+    const float x = __builtin_ldexpf(kLargest<T>, -power);      // (codes lie 2^-9 apart below 2^-6, else an eighth of a power of two)
+    return __builtin_ldexpf(x < 0x1p-6f ? floorf(x * 512.f) * 0x1p-9f : fminf(as_f32(as_u32(x) & 0xfff00000u), 448.f), power);
+  }
   // the least power of two that reaches x with a code of 448 = 1.75 * 2^8; 0 and subnormal numbers: one of -126 and less
   static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 135 + ((as_u32(x) & 0x7fffffu) > 0x600000u); }
   // the codes of four numbers over 2^power (pack), of four of T as they lie in memory (pack_words): rounded once, to the nearest and the even one of two
@@ -36,7 +41,7 @@ struct E4m3 {
 };
 
 struct Int8 {
-  template <typename T> static constexpr float kMost = __is_same(T, f16_t) ? 64512.f : 0x1.f8p+127f;
+  template <typename T> static __device__ __forceinline__ float most(int power) { return __builtin_ldexpf(fminf(floorf(__builtin_ldexpf(kLargest<T>, -power)), 127.f), power); }
   // 127 = 1.984375 * 2^6
   static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 133 + ((as_u32(x) & 0x7fffffu) > 0x7e0000u); }
   // 1.5 * 2^23 more leaves the nearest whole number, the even one of two, in the number's last bits

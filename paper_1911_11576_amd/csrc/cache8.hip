@@ -77,20 +77,19 @@ template <typename T> __device__ __forceinline__ float top_number(uint32_t bits)
     else return f16_to_f32(b);
   }
 }
-// The codes of 8 numbers over 2^power; CUT: no larger than what a code of T may stand for.
-template <typename T, class Code, bool CUT> __device__ __forceinline__ u32x2 codes_of(const Raw8<T>& r, int power) {
+// The codes of 8 numbers over 2^power; CUT: those beyond `limit` as that, the largest number of T that such a code stands for.
+template <typename T, class Code, bool CUT> __device__ __forceinline__ u32x2 codes_of(const Raw8<T>& r, int power, float limit) {
   if constexpr (sizeof(T) == 2 && !CUT) {
     return u32x2{Code::template pack_words<T>(r.w[0][0], r.w[0][1], power), Code::template pack_words<T>(r.w[0][2], r.w[0][3], power)};
   } else {
     constexpr int V = Vec<T>::V;
-    constexpr float kMost = Code::template kMost<T>;
     float x[8];
 #pragma unroll
     for (int i = 0; i < 8 / V; ++i) {
       float y[V];
       Vec<T>::unpack(r.w[i], y);
 #pragma unroll
-      for (int j = 0; j < V; ++j) x[V * i + j] = CUT ? __builtin_amdgcn_fmed3f(y[j], -kMost, kMost) : y[j];
+      for (int j = 0; j < V; ++j) x[V * i + j] = CUT ? copysignf(fminf(fabsf(y[j]), limit), y[j]) : y[j];
     }
     return u32x2{Code::pack(x[0], x[1], x[2], x[3], power), Code::pack(x[4], x[5], x[6], x[7], power)};
   }
@@ -211,9 +210,10 @@ template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_b
       }
     }
     // ---- the new ones
+    const float limit = Code::template most<T>(power);
     auto put = [&](auto cut) __attribute__((always_inline)) {
       auto one = [&](int r, const Raw8<T>& raw) __attribute__((always_inline)) {
-        u32x2 c = codes_of<T, Code, decltype(cut)::value>(raw, power);
+        u32x2 c = codes_of<T, Code, decltype(cut)::value>(raw, power, limit);
         if (decltype(cut)::value && nan) c = u32x2{0u, 0u};
         *reinterpret_cast<u32x2*>(codes + (int64_t)(lo + r) * a.cache.slot + 8 * p) = c;
       };
@@ -222,7 +222,7 @@ template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_b
         if (r0 + i * rows < last) one(r0 + i * rows, x[i]);
       for (int r = N * rows; r0 + r < last; r += rows) one(r0 + r, load8<T, ONCE>(row_at(r)));
     };
-    if (nan || most > Code::template kMost<T>) put(std::true_type{});
+    if (nan || most > limit) put(std::true_type{});
     else put(std::false_type{});
     if (t == 0) *scale_at = now;
   }

@@ -128,3 +128,20 @@ def test_oracle_store_grows_a_block():
     assert np.isnan(c[1][2, 0]) and np.isnan(paged8.numbers(*c, "e4m3")[2]).all()
     rows, mine = paged8.read(paged8.numbers(*b, "e4m3"), [[2, 1], [7, 0]], [5, 3], [0, 2, 3], 4)
     assert mine.tolist() == [True, True, True, False] and rows[0, 0, 0] == 1.0 and rows[1, 0, 0] == 0.125 and (rows[2] == 0).all()
+
+
+@pytest.mark.parametrize("code", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype, top, powers, numbers", [("f16", 65504.0, range(8, 27), 65504.0 - 32 * np.arange(1000)), ("bf16", 2.0**127 * (2 - 2.0**-7), range(120, 128), 2.0**120 * np.arange(60, 256))])
+def test_oracle_cuts_only_what_would_be_infinite(code, dtype, top, powers, numbers):
+    """Of fp16's numbers the greatest int8 code under 2^9 stands for 65024, which is one; under 2^11 63.5 and more would round to one that is none."""
+    every = np.sort(paged8.values(np.arange(128, dtype=np.uint8), code)[:127 if code == "e4m3" else 128])
+    for power in powers:
+        x = numbers[numbers <= every[-1] * 2.0**power]
+        if not len(x):
+            continue
+        codes, scales = np.zeros((1, 1, 8, len(x)), np.uint8), np.array([[2.0**power]])
+        got, scale = paged8.store(np.stack([x, -x])[:, None], codes, scales, [[0]], [3], [0, 2], code, dtype)
+        assert scale[0, 0] == 2.0**power
+        nearest = paged8.values(paged8.coded(x / 2.0**power, code), code)
+        want = np.where(nearest * 2.0**power > top, every[every * 2.0**power <= top].max(), nearest)
+        assert np.array_equal(paged8.values(got[0, 0, 1], code), want) and np.array_equal(paged8.values(got[0, 0, 2], code), -want)
