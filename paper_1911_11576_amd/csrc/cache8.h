@@ -38,18 +38,32 @@ struct E4m3 {
     const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)c, true);
     x[0] = lo[0]; x[1] = lo[1]; x[2] = hi[0]; x[3] = hi[1];
   }
+  // Four codes times `ratio`, as codes.  A product of 28 bits is rounded to the one of its two neighbours in fp32 whose last bit is 1, so that the rounding to a
+  // code's four bits is that of the product itself, next to the middle of two codes too.
+  static __device__ __forceinline__ uint32_t times(uint32_t c, float ratio) {
+    float x[4];
+    unpack(c, x);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float p = x[i] * ratio, left = fmaf(x[i], ratio, -p);
+      const uint32_t u = as_u32(p);
+      if (left != 0.f && !(u & 1)) x[i] = as_f32((left > 0.f) == (p > 0.f) ? u + 1 : u - 1);
+      else x[i] = p;
+    }
+    return pack(x[0], x[1], x[2], x[3], 0);
+  }
 };
 
 struct Int8 {
   template <typename T> static __device__ __forceinline__ float most(int power) { return __builtin_ldexpf(fminf(floorf(__builtin_ldexpf(kLargest<T>, -power)), 127.f), power); }
   // 127 = 1.984375 * 2^6
   static __device__ __forceinline__ int power(float x) { return (int)(as_u32(x) >> 23) - 133 + ((as_u32(x) & 0x7fffffu) > 0x7e0000u); }
-  // 1.5 * 2^23 more leaves the nearest whole number, the even one of two, in the number's last bits
-  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d, int power) {
-    const float s = __builtin_ldexpf(1.f, -power);
+  // four numbers times s, rounded once: 1.5 * 2^23 more leaves the nearest whole number, the even one of two, in the number's last bits
+  static __device__ __forceinline__ uint32_t whole(float a, float b, float c, float d, float s) {
     const uint32_t w0 = as_u32(fmaf(a, s, 0x1.8p23f)), w1 = as_u32(fmaf(b, s, 0x1.8p23f)), w2 = as_u32(fmaf(c, s, 0x1.8p23f)), w3 = as_u32(fmaf(d, s, 0x1.8p23f));
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(w3, w2, 0x0c0c0400u), __builtin_amdgcn_perm(w1, w0, 0x0c0c0400u), 0x05040100u);
   }
+  static __device__ __forceinline__ uint32_t pack(float a, float b, float c, float d, int power) { return whole(a, b, c, d, __builtin_ldexpf(1.f, -power)); }
   template <typename T> static __device__ __forceinline__ uint32_t pack_words(uint32_t a, uint32_t b, int power) {
     if constexpr (__is_same(T, bf16_t)) return pack(bf16_to_f32(a & 0xffffu), as_f32(a & 0xffff0000u), bf16_to_f32(b & 0xffffu), as_f32(b & 0xffff0000u), power);
     else return pack(f16_to_f32(a & 0xffffu), f16_to_f32(a >> 16), f16_to_f32(b & 0xffffu), f16_to_f32(b >> 16), power);
@@ -57,6 +71,11 @@ struct Int8 {
   static __device__ __forceinline__ void unpack(uint32_t c, float (&x)[4]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[i] = (float)(int8_t)(c >> (8 * i));
+  }
+  static __device__ __forceinline__ uint32_t times(uint32_t c, float ratio) {
+    float x[4];
+    unpack(c, x);
+    return whole(x[0], x[1], x[2], x[3], ratio);
   }
 };
 

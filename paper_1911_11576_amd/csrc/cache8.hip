@@ -200,11 +200,7 @@ template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_b
           if (r + u * rows >= lo) continue;
           u32x2 codes_now;
 #pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float z[4];
-            Code::unpack(was[u][i], z);
-            codes_now[i] = Code::pack(z[0] * ratio, z[1] * ratio, z[2] * ratio, z[3] * ratio, 0);
-          }
+          for (int i = 0; i < 2; ++i) codes_now[i] = Code::times(was[u][i], ratio);
           *reinterpret_cast<u32x2*>(codes + (int64_t)(r + u * rows) * a.cache.slot + 8 * p) = codes_now;
         }
       }
