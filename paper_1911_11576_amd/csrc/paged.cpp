@@ -201,8 +201,7 @@ fs_status create_cache8(const char* what, const fs_cache8_desc* desc, bool store
     g.out = store ? cache : rows;
     const int64_t touched = std::min<int64_t>((t >> shift) + 2 * b, d.blocks);
     g.bytes = 2 * t * row * (e + 1) + 8 * touched * d.kv_heads + 4 * (2 * b + touched);
-    if (store) p->lds_bytes = 16;
-    else p->lds_bytes = 768;
+    if (store && s.waves > 1) p->lds_bytes = 16;      // a maximum of each
     p->description = store ? numbers("cache_store8[GRID-CTA,WARP] wavefronts to a block and head=%lld; cta_num=%lld, cta_size=256", s.waves, 8ll * s.grid_groups * s.grid)
                            : numbers("cache_read8[GRID-CTA,THREAD] rows=%lld; cta_num=%lld, cta_size=256", s.groups, s.grid);
     return true;

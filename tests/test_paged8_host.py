@@ -145,3 +145,12 @@ def test_oracle_cuts_only_what_would_be_infinite(code, dtype, top, powers, numbe
         nearest = paged8.values(paged8.coded(x / 2.0**power, code), code)
         want = np.where(nearest * 2.0**power > top, every[every * 2.0**power <= top].max(), nearest)
         assert np.array_equal(paged8.values(got[0, 0, 1], code), want) and np.array_equal(paged8.values(got[0, 0, 2], code), -want)
+
+
+@pytest.mark.parametrize("change, shared", [({}, 0), (dict(tokens=5000, block_size=64), 0), (dict(tokens=5000, block_size=128), 16), (dict(kv_heads=1, head_dim=16), 0)])
+def test_shared_memory_of_store_and_read(change, shared):
+    """A maximum of each of four wavefronts, where a block has more new tokens than one holds (64 rows of 64 numbers); the read has none."""
+    with Plan.cache_read8(**dict(CACHE, **change)) as p:
+        assert p.info()["lds_bytes"] == 0
+    with Plan.cache_store8(**dict(CACHE, **change)) as p:
+        assert p.info()["lds_bytes"] == shared and ("head=4" if shared else "head=1") in p.describe()
