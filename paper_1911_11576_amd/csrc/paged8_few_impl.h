@@ -142,7 +142,8 @@ template <typename T, class Code, int D, int NT, int W, int KT, bool ONCE> __dev
       float kscale[TT], vscale[TT];      // of keys 16 t + 4 g + 0 .. 3, which are of one block
 #pragma unroll
       for (int t = 0; t < TT; ++t) {
-        kscale[t] = kscales[16 * t + 4 * g] * a.scale2;
+        const float f = kscales[16 * t + 4 * g] * a.scale2;
+        kscale[t] = fmaf(f, 0.f, f);      // infinite: NaN, or a dot below 0 would leave the key without a weight and the result a number
         vscale[t] = vscales[16 * t + 4 * g];
       }
       // fp16, where a row may not see every key: also that of the values of key `lane`, since bring_k has the scales of a later step written to their place

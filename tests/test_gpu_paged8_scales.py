@@ -1,7 +1,8 @@
-"""Attention over the paged cache in 8 bits where a step of the few-rows kernel whose keys not every row sees has another step behind it: in front of a window, and
-around blocks that are none.  The scales of the two steps must not be taken for each other's.  Tolerances as in test_gpu_paged8.py.
+"""Attention over the paged cache in 8 bits: scales of blocks that not every row sees, scales that are none, numbers beyond fp16's range, rows of nobody.  Tolerances as in
+test_gpu_paged8.py.
 
-A step is 32 or 64 keys of each of four or eight wavefronts, so a wavefront has a step behind a masked one in windows of 256 keys and more.
+The first tests are of steps of the few-rows kernel whose keys not every row sees and which have another step behind them, in front of a window and around blocks that are
+none: the scales of the two steps must not be taken for each other's.  A step is 32 or 64 keys of each of four or eight wavefronts, so a wavefront has a step behind a masked one in windows of 256 keys and more.
 """
 import numpy as np
 import pytest
@@ -9,7 +10,7 @@ import torch
 
 from oracle import paged8
 from test_gpu_paged import f64
-from test_gpu_paged8 import CODES, buffers, check_attention, inputs, plan_of, problem
+from test_gpu_paged8 import CODES, buffers, check_attention, check_out, inputs, plan_of, problem, wanted
 
 pytestmark = pytest.mark.gpu
 
@@ -114,3 +115,35 @@ def test_blocks_that_are_none_in_the_middle(new, q_heads, heads, dim, keys, wind
     rng = np.random.default_rng(keys)
     c["tables"] = np.where(rng.random(c["tables"].shape) < 1 / 6, rng.choice([-1, len(c["codes"][0]), 2**31 - 1], c["tables"].shape), c["tables"])
     check_attention(c, window, True, 0 if chunk else new)
+
+
+def launched(c, **kw):
+    plan, nbytes = plan_of(c, **kw)
+    with plan:
+        outs = buffers(c, nbytes)
+        plan.launch(inputs(c), outs)
+        torch.cuda.synchronize()
+    return outs
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("which", [0, 1], ids=["keys", "values"])
+@pytest.mark.parametrize("new, keys", [(1, 30), (3, 50), (2, 900), (70, 210), (150, 166)])
+def test_infinite_scale_of_the_last_block(dtype, code, which, new, keys):
+    """Rows that see it: not a number wherever the definition has none there, and an infinity where it has one (or NaN, where the weight is rounded to 0).  Rows before: as
+    without it."""
+    c = problem(9, dtype, code, [keys], [new], 4, 2, 64, 16)
+    first = (keys - 1) // 16 * 16
+    c["scales"][which][c["tables"][0, first // 16]] = np.inf
+    outs = launched(c, max_new=new)
+    before = max(0, new - (keys - first))
+    if before:
+        clean = dict(c, starts=np.array([0, before]), lengths=np.array([first]), q=c["q"][:before])
+        check_out(clean, [o[:before] for o in outs[:2]], wanted(clean), "rows before")
+    with np.errstate(invalid="ignore"):
+        want = wanted(c)[0][before:]
+    got, none = f64(outs[0])[before:], ~np.isfinite(want)
+    assert none.all() and not np.isfinite(got).any()
+    inf = np.isinf(want)
+    assert (np.isnan(got[inf]) | (got[inf] == want[inf])).all()
