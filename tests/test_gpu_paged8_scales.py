@@ -147,3 +147,34 @@ def test_infinite_scale_of_the_last_block(dtype, code, which, new, keys):
     assert none.all() and not np.isfinite(got).any()
     inf = np.isinf(want)
     assert (np.isnan(got[inf]) | (got[inf] == want[inf])).all()
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("new, keys", [(1, 30), (2, 100), (3, 900), (90, 300)])
+def test_values_beyond_fp16_are_infinite_or_right(code, new, keys):
+    """One key of the last block has values of 4 * 2^14 or 100 * 2^14 in every other column: an infinity there, or the sum that the numbers have; elsewhere nothing."""
+    c = problem(10, "f16", code, [keys], [new], 4, 2, 64, 16)
+    first = (keys - 1) // 16 * 16
+    last = c["tables"][0, first // 16]
+    c["scales"][1][last] = 2.0**14
+    c["codes"][1][last] = 0
+    c["codes"][1][last][:, 0, ::2] = 0x48 if code == "e4m3" else 100
+    outs, want = launched(c, max_new=new), wanted(c)
+    got, exact, weight, small = f64(outs[0]), want[0], want[2], want[3]
+    before = max(0, new - (keys - first))
+    off = (64 + 12) * 2.0**-24 * want[4] + 2.0**-20
+    room = (2.0**-11 + 2 * off[..., None]) * weight + 2.0**-25 * small + 2.0**-11 * np.abs(exact) + 2.0**-25
+    right = (np.abs(got - exact) <= room) | (np.isposinf(got) & (exact + room >= 65520))
+    assert right[:before].all() and right[:, :, 1::2].all()
+    assert (right | np.isposinf(got)).all()
+
+
+@pytest.mark.parametrize("max_new", [0, 1])
+@pytest.mark.parametrize("starts, nobody", [([5, 5, 1, 9], [0]), ([3, 1, 5, 6], [0, 6, 7, 8]), ([2, 4, 4, 7], [0, 1, 7, 8])])
+def test_rows_of_no_request_stay(starts, nobody, max_new):
+    c = problem(7, "bf16", "e4m3", [20, 300, 64], [3, 3, 3], 8, 2, 64, 16)
+    c["starts"] = np.array(starts)
+    outs = launched(c, max_new=max_new)
+    assert (outs[0][nobody] == 3).all() and (outs[1][nobody] == 3).all()
+    others = np.setdiff1d(np.arange(9), nobody)
+    assert (outs[0][others] != 3).any(dim=2).all()
