@@ -206,8 +206,8 @@ template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_b
       }
     }
     // ---- the new ones
-    const float limit = Code::template most<T>(power);
     auto put = [&](auto cut) __attribute__((always_inline)) {
+      const float limit = decltype(cut)::value ? Code::template most<T>(power) : 0.f;
       auto one = [&](int r, const Raw8<T>& raw) __attribute__((always_inline)) {
         u32x2 c = codes_of<T, Code, decltype(cut)::value>(raw, power, limit);
         if (decltype(cut)::value && nan) c = u32x2{0u, 0u};
@@ -218,7 +218,8 @@ template <typename T, class Code, int W, int N, bool ONCE> __global__ __launch_b
         if (r0 + i * rows < last) one(r0 + i * rows, x[i]);
       for (int r = N * rows; r0 + r < last; r += rows) one(r0 + r, load8<T, ONCE>(row_at(r)));
     };
-    if (nan || most > limit) put(std::true_type{});
+    // (no code stands for more than twice its number, whatever the scale)
+    if (nan || most >= (__is_same(T, f16_t) ? 0x1p15f : 0x1p127f)) put(std::true_type{});
     else put(std::false_type{});
     if (t == 0) *scale_at = now;
   }
