@@ -521,13 +521,13 @@ typedef enum { FS_CODE_E4M3 = 0, FS_CODE_INT8 = 1 } fs_code;
 /* New keys and values quantised as they are written.  Request b's new tokens are rows starts[b] .. starts[b+1]-1 of k and v and the last of
  * its lengths[b] tokens (what block tables give, and attention takes).  For every block that they touch and every head
  *     need = the least power of two s, 2^-126 or more, with |x| <= largest code * s for the block's new numbers x
- *     scale = need, where the block's first token is new; else the larger of need and the scale from before, up to a power of two
+ *     scale = need, where the block's first token is new; else the larger of need and the scale from before (its size), up to a power of two
  *     codes of the block's tokens from before, where that scale has changed: c * before / scale; of the new ones: x / scale; rounded to the
  *     nearest, the even one of two
- * Powers of two: c * scale is exact in every type, a block that grows loses of e4m3 codes only what falls below their least numbers, and of whole numbers, over all
- * its growth, less than one step of its last scale.  Numbers whose code would stand for an infinity of dtype are cut to the largest that does not.  A
- * new number that is infinite or NaN, or such a scale from before, makes the scale NaN: nothing of that block and head is a number then, until
- * the block begins anew.
+ * Powers of two: c * scale is exact in every type but at its least numbers (fp16 rounds below 2^-24: e4m3 from scales of 2^-16 on down, int8 of 2^-25; bf16 below 2^-133), a
+ * block that grows loses of e4m3 codes only what falls below their least numbers, and of whole numbers, over all its growth, less than one step of its last scale.  Numbers whose
+ * code over the block's scale would stand for an infinity of dtype are cut to the largest that does not.  A new number that is infinite or NaN, or a scale from before that is,
+ * or is beyond 2^127, makes the scale NaN: nothing of that block and head is a number then, until the block begins anew.
  *   inputs    k, v [tokens, kv_heads, head_dim], tables i32 [requests, table_blocks], lengths i32 [requests], starts i32 [requests+1]
  *   outputs   k_cache, v_cache, k_scales, v_scales (read and written)
  * Nothing is written for rows of no request or before a request's first token, for blocks outside [0, blocks), and in other places of a block than those of the request's tokens.  Two
@@ -554,8 +554,9 @@ fs_status fs_plan_create_cache_read8(const fs_cache8_desc* desc, fs_plan** out);
 /* Attention of new tokens over the cache in 8 bits: fs_plan_create_paged_attention with the numbers that the codes stand for as keys and values.
  *   inputs    q, k_cache, v_cache, k_scales, v_scales, tables, lengths, starts
  *   outputs   out; with log_sum_exp also lse; with partial_bytes not 0 also the partial results
- * Any scales are taken: where one is no power of two, the numbers of its block may be rounded to dtype, as keys and values held in dtype had been; numbers beyond the
- * range of dtype may count as infinities.  What is said there of masks, blocks outside, lengths, rows of no request and NaN holds here, of scales too: one of
+ * Any scales are taken: where one is no power of two, or so small that dtype does not hold all that its codes stand for, the numbers of its block may be rounded to dtype, as keys
+ * and values held in dtype had been; numbers beyond the range of dtype may count as infinities, an infinite scale of keys as NaN.  Queries in bf16 are to be below 2^112: their
+ * product with the codes may be summed up before the scale.  What is said there of masks, blocks outside, lengths, rows of no request and NaN holds here, of scales too: one of
  * a block that a row does not see never reaches it.  block_size 8 to 1024, strides of the cache multiples of 16 codes; limits and errors are the same. */
 typedef struct {
   int32_t dtype, code;             /* FS_F16 or FS_BF16: q, out; fs_code: the caches */

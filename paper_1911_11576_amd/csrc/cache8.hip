@@ -235,7 +235,7 @@ template <typename T, class Code, bool ONCE> void store_launch(const Cache8Args&
 
 // A wavefront has a.groups rows (tokens).  Where each one's codes lie is found a row a lane; then the wavefront goes over the columns, 8 codes to a lane, which
 // are the same in all of its rows, K columns of U rows requested together.  WIDE: a token has 64 times 8 codes and more; else several rows lie side by side.
-// 5.7 TB/s for 118997 tokens of 8 heads of 128, K and V (129 us; with one column of 4 rows at a time 142, of 8 rows 146, a workgroup's rows found by one wavefront in
+// 5.5 TB/s for 118997 tokens of 8 heads of 128, K and V (134 us, in some runs 129; with one column of 4 rows at a time 142, of 8 rows 146, a workgroup's rows found by one wavefront in
 // LDS 140, its items one behind the other, each with divisions of its own, 182; stores through the caches 156 instead of 141).
 template <typename T, class Code, bool WIDE> __global__ __launch_bounds__(256) void cache8_read_kernel(const Cache8Args a) {
   constexpr int U = 2, K = 4;

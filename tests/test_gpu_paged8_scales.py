@@ -178,3 +178,21 @@ def test_rows_of_no_request_stay(starts, nobody, max_new):
     assert (outs[0][nobody] == 3).all() and (outs[1][nobody] == 3).all()
     others = np.setdiff1d(np.arange(9), nobody)
     assert (outs[0][others] != 3).any(dim=2).all()
+
+
+@pytest.mark.parametrize("code", CODES)
+@pytest.mark.parametrize("dtype, powers", [("f16", (-20, -14)), ("f16", (-32, -20)), ("bf16", (-100, -90)), ("bf16", (-126, -117))])
+@pytest.mark.parametrize("new, keys, dim", [(1, 300, 128), (3, 900, 64), (90, 300, 128), (40, 100, 32)])
+def test_small_scales(dtype, powers, code, new, keys, dim):
+    """Powers of two with which fp16 does not hold all that the codes stand for: keys and values may be rounded to it, 2^-25 of each at its end.  And the least that a
+    store makes, in bf16."""
+    c = problem(21, dtype, code, [keys, keys // 2], [new, 1], 4, 2, dim, 16)
+    rng = np.random.default_rng(keys)
+    for s in c["scales"]:
+        there = np.isfinite(s)
+        s[there] = 2.0 ** rng.integers(*powers, there.sum())
+    c["powers"] = dtype == "bf16"
+    outs, want = launched(c, max_new=new), list(wanted(c))
+    if dtype == "f16":      # a score, by as much of every key
+        want[4] = want[4] + c["scale"] * np.abs(f64(c["q"])).sum(2) * 2.0**-25 / 2.0**-11
+    check_out(c, outs, want)
